@@ -418,6 +418,186 @@ dard_status dard_commit_remask(int phase, const dard_params* params, int b, int 
     return DARD_OK;
 }
 
+// ---------------------------------------------------------------- microscaled formats
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Arguments that the MX calls have in common.
+int check_mx_types(int format, int dtype) {
+    if (format != DARD_MX_FP8 && format != DARD_MX_FP4) return fail(DARD_ERR_ARG, "unknown MX format %d", format);
+    if (dtype != DARD_DTYPE_F32 && dtype != DARD_DTYPE_BF16) return fail(DARD_ERR_ARG, "unknown dtype %d", dtype);
+    return DARD_OK;
+}
+
+int check_mx_rows(const void* x, int dtype, int64_t ld, int rows, int K, const void* codes, const void* scales) {
+    if (!x || !codes || !scales) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (rows < 1 || K < 32 || K % 32 || ld < K) return fail(DARD_ERR_SHAPE, "need rows >= 1, K %% 32 == 0, ld >= K");
+    if ((int64_t)rows * (K / 8) > 0x7FFFFFFFll) return fail(DARD_ERR_SHAPE, "rows * K must be under 2^34");
+    if (!aligned(codes, 16)) return fail(DARD_ERR_ARG, "codes must be 16-byte aligned");
+    if (!aligned(x, esize(dtype))) return fail(DARD_ERR_ARG, "x must be aligned to its element");
+    return DARD_OK;
+}
+
+int check_mx_cache(const void* kc, const void* ks, const void* vc, const void* vs, int b, int Hkv, int dh, int cap) {
+    if (!kc || !ks || !vc || !vs) return fail(DARD_ERR_ARG, "NULL cache pointer");
+    if (dh != 64 && dh != 128) return fail(DARD_ERR_SHAPE, "dh must be 64 or 128");
+    if (b < 1 || Hkv < 1 || cap < 32 || cap % 32) return fail(DARD_ERR_SHAPE, "need b, Hkv >= 1 and cap %% 32 == 0");
+    if (!aligned(kc, 16) || !aligned(vc, 16) || !aligned(ks, 8) || !aligned(vs, 8))
+        return fail(DARD_ERR_ARG, "cache codes must be 16-byte aligned, scales 8-byte");
+    return DARD_OK;
+}
+
+int check_mx_kv(int dtype, const void* k, const void* v, int64_t ld, const void* kc, const void* ks, const void* vc,
+                const void* vs, int b, int n, int Hkv, int dh, int pos, int cap) {
+    if (int rc = check_mx_types(DARD_MX_FP4, dtype)) return rc;
+    if (!k || !v) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (int rc = check_mx_cache(kc, ks, vc, vs, b, Hkv, dh, cap)) return rc;
+    if (n < 1 || pos < 0 || n > cap || pos > cap - n || ld < (int64_t)Hkv * dh)
+        return fail(DARD_ERR_SHAPE, "need n >= 1, pos >= 0, pos + n <= cap, ld >= Hkv * dh");
+    if ((double)b * n * Hkv * (dh / 8) > 2147483647.0) return fail(DARD_ERR_SHAPE, "too many new keys in one call");
+    if (!aligned(k, esize(dtype)) || !aligned(v, esize(dtype))) return fail(DARD_ERR_ARG, "k and v must be aligned to their element");
+    return DARD_OK;
+}
+
+}  // namespace
+
+dard_status dard_quantize_mx(int dtype, const void* x, int64_t ld, int rows, int K, int format, void* codes,
+                             uint8_t* scales, void* stream) {
+    if (int rc = check_mx_types(format, dtype)) return rc;
+    if (int rc = check_mx_rows(x, dtype, ld, rows, K, codes, scales)) return rc;
+    HIPOK(launch_quantize_mx(dtype, x, ld, rows, K, format, (uint8_t*)codes, scales, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+dard_status dard_dequantize_mx(int format, const void* codes, const uint8_t* scales, int rows, int K, int dtype, void* x,
+                               int64_t ld, void* stream) {
+    if (int rc = check_mx_types(format, dtype)) return rc;
+    if (int rc = check_mx_rows(x, dtype, ld, rows, K, codes, scales)) return rc;
+    HIPOK(launch_dequantize_mx(format, (const uint8_t*)codes, scales, rows, K, dtype, x, ld, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+dard_status dard_resid_norm_mx(float* h, int delta_dtype, const void* delta, int gain_dtype, const void* gain, float eps,
+                               int rows, int d, int format, void* codes, uint8_t* scales, void* stream) {
+    if (int rc = check_mx_types(format, gain_dtype)) return rc;
+    if (delta && (delta_dtype != DARD_DTYPE_F32 && delta_dtype != DARD_DTYPE_BF16))
+        return fail(DARD_ERR_ARG, "unknown dtype %d", delta_dtype);
+    if (!gain) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (!(eps >= 0.f)) return fail(DARD_ERR_ARG, "need eps >= 0");
+    if (int rc = check_mx_rows(h, DARD_DTYPE_F32, d, rows, d, codes, scales)) return rc;
+    if (d > 8192) return fail(DARD_ERR_SHAPE, "d must be <= 8192");
+    if (!aligned(gain, esize(gain_dtype)) || (delta && !aligned(delta, esize(delta_dtype))))
+        return fail(DARD_ERR_ARG, "gain and delta must be aligned to their element");
+    TraceScope ts(DARD_K_NORM, (hipStream_t)stream);
+    HIPOK(launch_resid_norm_mx(h, delta_dtype, delta, gain_dtype, gain, eps, rows, d, format, (uint8_t*)codes, scales,
+                               (hipStream_t)stream));
+    return DARD_OK;
+}
+
+namespace {
+
+int check_mx_weight(int N, int K) {
+    if (N < 1 || K < 32 || K % 32) return fail(DARD_ERR_SHAPE, "need N >= 1 and K %% 32 == 0");
+    const MxPacked p = mx_packed(N, K);
+    if (p.scales > 0x7FFFFFFFull) return fail(DARD_ERR_SHAPE, "the packed codes of a weight must be under 2 GiB");
+    return DARD_OK;
+}
+
+}  // namespace
+
+size_t dard_packed_mx_bytes(int N, int K) { return check_mx_weight(N, K) ? 0 : mx_packed(N, K).total; }
+
+dard_status dard_pack_matrix_mx(const void* codes, const uint8_t* scales, int N, int K, void* Wp, void* stream) {
+    if (!codes || !scales || !Wp) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (int rc = check_mx_weight(N, K)) return rc;
+    if (!aligned(codes, 16) || !aligned(Wp, 16)) return fail(DARD_ERR_ARG, "codes and Wp must be 16-byte aligned");
+    HIPOK(launch_pack_mx(codes, scales, N, K, Wp, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+size_t dard_linear_mx_workspace_bytes(int format, int M, int N, int K) {
+    if (check_mx_types(format, DARD_DTYPE_F32) || M < 1 || check_mx_weight(N, K)) return 0;
+    return linear_mx_partial_bytes(format, M, N, K);
+}
+
+dard_status dard_linear_mx(int format, const void* codes, const uint8_t* scales, int M, int K, const void* Wp, int N,
+                           int out_dtype, void* Y, void* ws, size_t ws_bytes, void* stream) {
+    if (int rc = check_mx_types(format, out_dtype)) return rc;
+    if (!codes || !scales || !Wp || !Y) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (M < 1) return fail(DARD_ERR_SHAPE, "need M >= 1");
+    if (int rc = check_mx_weight(N, K)) return rc;
+    if (!aligned(codes, 16) || !aligned(Wp, 16)) return fail(DARD_ERR_ARG, "codes and Wp must be 16-byte aligned");
+    if (!aligned(Y, esize(out_dtype))) return fail(DARD_ERR_ARG, "Y must be aligned to its element");
+    const size_t need = linear_mx_partial_bytes(format, M, N, K);
+    if (need && (!ws || ws_bytes < need)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", need);
+    if (need && !aligned(ws, 16)) return fail(DARD_ERR_ARG, "the workspace must be 16-byte aligned");
+    HIPOK(launch_linear_mx(format, (const uint8_t*)codes, scales, M, K, Wp, N, out_dtype, Y, (float*)ws,
+                           (hipStream_t)stream));
+    return DARD_OK;
+}
+
+dard_status dard_kv_write_mx(int dtype, const void* k, const void* v, int64_t ld, int b, int n, int Hkv, int dh, int pos,
+                             const int32_t* prefix, int cap, void* kc, uint8_t* ks, void* vc, uint8_t* vs, void* stream) {
+    if (int rc = check_mx_kv(dtype, k, v, ld, kc, ks, vc, vs, b, n, Hkv, dh, pos, cap)) return rc;
+    MxKvArgs a{};
+    a.kc = (uint8_t*)kc; a.ks = ks; a.vc = (uint8_t*)vc; a.vs = vs;
+    a.prefix = prefix; a.b = b; a.n = n; a.Hkv = Hkv; a.dh = dh; a.cap = cap; a.pos = pos; a.ld = ld;
+    HIPOK(launch_kv_write_mx(dtype, a, k, v, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+dard_status dard_kv_read_mx(const void* kc, const uint8_t* ks, const void* vc, const uint8_t* vs, int cap, int b, int n,
+                            int Hkv, int dh, int pos, const int32_t* prefix, int dtype, void* k, void* v, int64_t ld,
+                            void* stream) {
+    if (int rc = check_mx_kv(dtype, k, v, ld, kc, ks, vc, vs, b, n, Hkv, dh, pos, cap)) return rc;
+    MxKvArgs a{};
+    a.kc = (uint8_t*)kc; a.ks = (uint8_t*)ks; a.vc = (uint8_t*)vc; a.vs = (uint8_t*)vs;   // (read only)
+    a.prefix = prefix; a.b = b; a.n = n; a.Hkv = Hkv; a.dh = dh; a.cap = cap; a.pos = pos; a.ld = ld;
+    HIPOK(launch_kv_read_mx(dtype, a, k, v, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+namespace {
+
+int check_mx_attention(int b, int B, int Hq, int Hkv, int dh, int P) {
+    if (b < 1 || B < 1 || B > 256 || P < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || P > 0x7FFFFFFF - 1024)
+        return fail(DARD_ERR_SHAPE, "bad attention shape (b=%d B=%d P=%d Hq=%d Hkv=%d)", b, B, P, Hq, Hkv);
+    if (dh != 64 && dh != 128) return fail(DARD_ERR_SHAPE, "dh must be 64 or 128");
+    if ((double)b * 2 * B * Hq * (dh / 4) > 2147483647.0) return fail(DARD_ERR_SHAPE, "too many query rows in one call");
+    return DARD_OK;
+}
+
+}  // namespace
+
+size_t dard_attention_mx_workspace_bytes(int b, int B, int Hq, int Hkv, int dh, int P) {
+    return check_mx_attention(b, B, Hq, Hkv, dh, P) ? 0 : attention_mx_partial_bytes(b, B, Hq, Hkv, dh, P);
+}
+
+dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_t* ks, const void* vc, const uint8_t* vs,
+                                     int P, const int32_t* prefix, int cap, const uint8_t* state, const float* conf,
+                                     int b, int B, int Hq, int Hkv, int dh, float scale, uint32_t flags, void* out,
+                                     void* ws, size_t ws_bytes, void* stream) {
+    if (!q || !state || !conf || !out) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (int rc = check_flags(flags)) return rc;
+    if (int rc = check_mx_attention(b, B, Hq, Hkv, dh, P)) return rc;
+    if (int rc = check_mx_cache(kc, ks, vc, vs, b, Hkv, dh, cap)) return rc;
+    if (2 * B > cap || P > cap - 2 * B) return fail(DARD_ERR_SHAPE, "P + 2B must be <= cap");
+    if (!aligned(q, 16) || !aligned(out, 16)) return fail(DARD_ERR_ARG, "q and out must be 16-byte aligned");
+    const size_t need = attention_mx_partial_bytes(b, B, Hq, Hkv, dh, P);
+    if (need && (!ws || ws_bytes < need)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", need);
+    if (need && !aligned(ws, 16)) return fail(DARD_ERR_ARG, "the workspace must be 16-byte aligned");
+    MxAttnArgs a{};
+    a.q = (const bf16_bits*)q; a.out = (bf16_bits*)out;
+    a.kc = (const uint8_t*)kc; a.ks = ks; a.vc = (const uint8_t*)vc; a.vs = vs;
+    a.state = state; a.conf = conf; a.prefix = prefix;
+    a.P = P; a.cap = cap; a.b = b; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.dh = dh;
+    a.scale = scale; a.flags = flags; a.part = (float*)ws;
+    TraceScope ts(DARD_K_ATTENTION, (hipStream_t)stream);
+    HIPOK(launch_attention_mx(a, (hipStream_t)stream));
+    return DARD_OK;
+}
+
 // ---------------------------------------------------------------- weights / KV
 size_t dard_packed_weight_bytes(const dard_dims* dims) {
     if (check_dims(dims)) return 0;

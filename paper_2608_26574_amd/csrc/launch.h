@@ -11,6 +11,8 @@
 
 namespace dard {
 
+typedef uint16_t bf16_bits;   // bfloat16 bit pattern
+
 // bf16 activations that feed a projection GEMM are stored fragment-major, in
 // the layout of the packed weights: the 16 x 64 block (m/16, k/64) is
 // contiguous, so every wave load (streaming GEMM) or tile copy (tiled
@@ -219,6 +221,60 @@ struct DecideArgs {
     float* dbg_entropy; float* dbg_margin;
 };
 hipError_t launch_decide(const DecideArgs& a, hipStream_t s);
+
+// ---- mx.hip, mx_linear.hip, mx_attention.hip (microscaled formats)
+// Packed MXFP4 weights [N][K]: rows in blocks of 32, K in blocks of 32 padded
+// to whole units of 256.  Codes: [nblk][KBp][32 rows][16 bytes]; scales, from
+// byte `scales` on: [nblk][KBp / 8][64 lanes][4 bytes], byte j of lane l the
+// scale of row l % 32 and k block 2 j + l / 32 of the unit.  Rows and k blocks
+// past N and K hold zeros.
+struct MxPacked {
+    int nblk, KBp;
+    size_t scales, total;
+};
+inline MxPacked mx_packed(int N, int K) {
+    MxPacked p;
+    p.nblk = (N + 31) / 32;
+    p.KBp = (K / 32 + 7) / 8 * 8;
+    p.scales = (size_t)p.nblk * p.KBp * 512;
+    p.total = p.scales + (size_t)p.nblk * p.KBp * 32;
+    return p;
+}
+hipError_t launch_quantize_mx(int dtype, const void* x, int64_t ld, int64_t rows, int K, int format, uint8_t* codes,
+                              uint8_t* scales, hipStream_t s);
+hipError_t launch_dequantize_mx(int format, const uint8_t* codes, const uint8_t* scales, int64_t rows, int K, int dtype,
+                                void* x, int64_t ld, hipStream_t s);
+hipError_t launch_resid_norm_mx(float* h, int delta_dtype, const void* delta, int gain_dtype, const void* gain, float eps,
+                                int rows, int d, int format, uint8_t* codes, uint8_t* scales, hipStream_t s);
+hipError_t launch_pack_mx(const void* codes, const uint8_t* scales, int N, int K, void* Wp, hipStream_t s);
+// Y = X W^T (float32 or bf16 [M][N]); part: room for the partials of a K split
+// over workgroups, linear_mx_partial_bytes() of it.
+size_t linear_mx_partial_bytes(int format, int M, int N, int K);
+hipError_t launch_linear_mx(int format, const uint8_t* xc, const uint8_t* xs, int M, int K, const void* Wp, int N,
+                            int out_dtype, void* y, float* part, hipStream_t s);
+// The MXFP4 cache of one layer: K codes [b][Hkv][cap][dh/2], scales
+// [b][Hkv][cap][dh/32]; V in groups of 8 keys, codes
+// [b][Hkv][cap/8][dh/4][8][2], scales [b][Hkv][cap/8][dh/32][8].
+struct MxKvArgs {
+    uint8_t* kc; uint8_t* ks; uint8_t* vc; uint8_t* vs;
+    const int32_t* prefix;   // per-sequence first position (clamped to [0, pos]), or NULL: pos
+    int b, n, Hkv, dh, cap, pos;
+    int64_t ld;              // elements between tokens of k / v
+};
+hipError_t launch_kv_write_mx(int dtype, const MxKvArgs& a, const void* k, const void* v, hipStream_t s);
+hipError_t launch_kv_read_mx(int dtype, const MxKvArgs& a, void* k, void* v, hipStream_t s);
+struct MxAttnArgs {
+    const bf16_bits* q; bf16_bits* out;   // [b][2B][Hq][dh]
+    const uint8_t* kc; const uint8_t* ks; const uint8_t* vc; const uint8_t* vs;
+    const uint8_t* state; const float* conf;   // [b][B]
+    const int32_t* prefix;                // [b] prefix lengths (clamped to [0, P]), or NULL: P
+    int P, cap, b, B, Hq, Hkv, dh;
+    float scale;
+    uint32_t flags;
+    float* part;                          // key-split partials (attention_mx_partial_bytes)
+};
+size_t attention_mx_partial_bytes(int b, int B, int Hq, int Hkv, int dh, int P);
+hipError_t launch_attention_mx(const MxAttnArgs& a, hipStream_t s);
 
 // ---- tracing (api.cpp)
 // While a TraceScope whose class is enabled (dard_trace_enable) is alive on

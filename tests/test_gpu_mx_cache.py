@@ -1,0 +1,376 @@
+"""The MXFP4 key/value cache and the state-masked attention over it, against
+plain float64 forms: layout and bytes of the writer exactly, the attention
+within the bound that its roundings give."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as R
+from oracle import dard_oracle as O
+from paper_2608_26574_amd import dard
+
+pytestmark = pytest.mark.gpu
+
+
+def announce(*a):
+    print("[case]", *a, file=sys.stderr, flush=True)
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def empty_cache(b, Hkv, cap, dh, fill):
+    full = lambda *n: np.full(n, fill, np.uint8)   # noqa: E731
+    return [full(b, Hkv, cap, dh // 2), full(b, Hkv, cap, dh // 32), full(b, Hkv, cap // 8, dh // 4, 8, 2),
+            full(b, Hkv, cap // 8, dh // 32, 8)]
+
+
+def written(cache, k, v, first):
+    """The cache after keys k, v [b][n][Hkv][dh] at first[s].. of every sequence."""
+    kc, ks, vc, vs = (t.copy() for t in cache)
+    rc, rs = R.rows_of_cache(vc, vs)
+    rc, rs = rc.copy(), rs.copy()
+    n = k.shape[1]
+    for s, p in enumerate(first):
+        for x, c, sc in ((k, kc, ks), (v, rc, rs)):
+            code, scale = R.quantize(x[s].transpose(1, 0, 2), R.FP4)
+            c[s, :, p:p + n], sc[s, :, p:p + n] = R.pack(code, R.FP4), scale
+    return [kc, ks, *R.grouped(rc, rs)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b,n,Hkv,dh,pos,cap,ragged", [
+    (1, 1, 1, 64, 0, 32, False), (1, 64, 32, 128, 609, 704, False), (2, 13, 4, 64, 5, 64, False),
+    (3, 37, 2, 128, 27, 64, True), (2, 96, 4, 128, 0, 96, False), (5, 8, 3, 64, 24, 32, True),
+    (1, 333, 2, 128, 3, 352, False), (4, 200, 4, 128, 11, 224, True)])
+def test_write_and_read(dtype, b, n, Hkv, dh, pos, cap, ragged):
+    announce("kv", dtype, b, n, Hkv, dh, pos, cap, ragged)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    wide = (torch.randn(b, n, 3 * Hkv + 1, dh, generator=g, device="cuda") * 2).to(dtype)
+    k, v = wide[:, :, Hkv:2 * Hkv], wide[:, :, 2 * Hkv:3 * Hkv]
+    first = [pos] * b
+    prefix = None
+    if ragged:   # lengths past the ends are taken as the ends
+        first = [-3, pos + 9] + [(7 * s) % (pos + 1) for s in range(b - 2)]
+        prefix = torch.tensor(first, dtype=torch.int32, device="cuda")
+        first = [min(max(p, 0), pos) for p in first]
+    start = empty_cache(b, Hkv, cap, dh, 0xFF)
+    cache = [dev(t) for t in start]
+    dard.dard_kv_write_mx(k, v, cache, pos, prefix=prefix)
+    want = written(start, k.double().cpu().numpy(), v.double().cpu().numpy(), first)
+    for name, got, ref in zip(("kc", "ks", "vc", "vs"), cache, want):
+        assert np.array_equal(got.cpu().numpy(), ref), name
+    back = torch.full((b, n, 2 * Hkv, dh), 9.0, dtype=dtype, device="cuda")
+    kb = back[:, :, :Hkv]
+    vb = torch.full((b, n, 2 * Hkv, dh), 9.0, dtype=dtype, device="cuda")[:, :, Hkv:]
+    dard.dard_kv_read_mx(cache, pos, kb, vb, prefix=prefix)
+    for x, y in ((k, kb), (v, vb)):
+        ref = R.values(*R.quantize(x.double().cpu().numpy(), R.FP4), R.FP4)
+        assert np.array_equal(y.double().cpu().numpy(), ref)
+    assert bool((back[:, :, Hkv:] == 9.0).all())
+
+
+def test_write_not_finite():
+    announce("kv not finite")
+    k = torch.randn(1, 9, 2, 64, device="cuda")
+    v = torch.randn(1, 9, 2, 64, device="cuda")
+    k[0, 3, 1, 40], v[0, 8, 0, 1] = float("inf"), float("nan")
+    cache = [dev(t) for t in empty_cache(1, 2, 32, 64, 0)]
+    dard.dard_kv_write_mx(k, v, cache, 1)
+    want = written(empty_cache(1, 2, 32, 64, 0), k.double().cpu().numpy(), v.double().cpu().numpy(), [1])
+    for got, ref in zip(cache, want):
+        assert np.array_equal(got.cpu().numpy(), ref)
+    kb, vb = torch.empty_like(k), torch.empty_like(v)
+    dard.dard_kv_read_mx(cache, 1, kb, vb)
+    nan_k, nan_v = torch.isnan(kb).cpu().numpy(), torch.isnan(vb).cpu().numpy()
+    assert nan_k[0, 3, 1, 32:].all() and nan_k.sum() == 32
+    assert nan_v[0, 8, 0, :32].all() and nan_v.sum() == 32
+
+
+# ------------------------------------------------------------------ attention
+def block(b, B, seed, frac=(0.4, 0.3)):
+    rng = np.random.default_rng(seed)
+    u = rng.random((b, B))
+    state = np.where(u < frac[0], O.STATE_M, np.where(u < frac[0] + frac[1], O.STATE_C, O.STATE_U)).astype(np.uint8)
+    conf = rng.random((b, B)).astype(np.float32)
+    if B > 3:
+        conf[:, 1] = conf[:, 3]   # tied candidates
+    return state, conf
+
+
+def visible(state, conf, P, flags):
+    """[2B][P + 2B] keys that the rows of one sequence see."""
+    B = len(state)
+    take = O.take_x(state, conf, flags)
+    return np.concatenate([np.ones((2 * B, P), bool), take, ~take], 1)
+
+
+def attend(q, k, v, seen, scale):
+    """(out, its largest error) of one head: q [R][dh], k, v [K][dh].
+
+    Probabilities are rounded to bf16 (2^-8 of each, while their sum is taken
+    before), and so is the output.  A score is a float32 sum of dh products,
+    off by at most dh 2^-23 sum |q k|, scaled and shifted (a few roundings of
+    it more), and exp2 is good to 2^-20; each of these moves a probability and the
+    sum it is divided by."""
+    k, v = np.where(np.isnan(k), 0, k), np.where(np.isnan(v), 0, v)
+    s = np.where(seen, q @ k.T * scale, -np.inf)
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    off = (q.shape[1] + 8) * 2.0 ** -23 * (np.abs(q) @ np.abs(k).T).max(-1, keepdims=True) * scale + 2.0 ** -20
+    return p @ v, (2.0 ** -7 + 2 * off) * (p @ np.abs(v)) + 1e-30
+
+
+def attention_case(b, B, P, Hq, Hkv, dh, flags=0, lens=None, seed=0, cap_extra=0, qstd=1.0, nan_key=None):
+    rng = np.random.default_rng(seed + 17 * B + P)
+    first = [P] * b if lens is None else [min(max(p, 0), P) for p in lens]
+    cap = -(-(P + 2 * B) // 32) * 32 + cap_extra
+    # keys that are not written hold NaN blocks
+    cache = empty_cache(b, Hkv, cap, dh, 0xFF)
+    kc, ks, rc, rs = cache[0], cache[1], *(t.copy() for t in R.rows_of_cache(cache[2], cache[3]))
+    kv = []
+    for s, p in enumerate(first):
+        n = p + 2 * B
+        pair = []
+        for c, sc in ((kc, ks), (rc, rs)):
+            code, scale = R.quantize(rng.standard_normal((Hkv, n, dh)), R.FP4)
+            if nan_key is not None:
+                scale[nan_key[0], p + nan_key[1], nan_key[2]] = 255
+            c[s, :, :n], sc[s, :, :n] = R.pack(code, R.FP4), scale
+            pair.append(R.values(code, scale, R.FP4))
+        kv.append(pair)
+    vc, vs = R.grouped(rc, rs)
+    state, conf = block(b, B, seed)
+    q = torch.from_numpy(rng.standard_normal((b, 2 * B, Hq, dh)) * qstd).bfloat16().cuda()
+    out = torch.full_like(q, float("nan"))
+    room = torch.full((dard.dard_attention_mx_workspace_bytes(b, B, Hq, Hkv, dh, P) // 4,), float("nan"), device="cuda")
+    prefix = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    dard.dard_masked_attention_mx(q, [dev(t) for t in (kc, ks, vc, vs)], P, dev(state), dev(conf), dh ** -0.5, flags, out,
+                                  ws=room, prefix=prefix)
+    got, qn = out.double().cpu().numpy(), q.double().cpu().numpy()
+    worst = 0.0
+    for s, p in enumerate(first):
+        seen = visible(state[s], conf[s], p, flags)
+        for h in range(Hq):
+            k, v = kv[s][0][h // (Hq // Hkv)], kv[s][1][h // (Hq // Hkv)]
+            ref, bound = attend(qn[s, :, h], k, v, seen, dh ** -0.5)
+            g = got[s, :, h]
+            if nan_key is not None and h // (Hq // Hkv) == nan_key[0]:
+                sees = seen[:, p + nan_key[1]]
+                assert np.isnan(g[sees]).all()   # a NaN score makes the whole row NaN
+                assert np.isfinite(g[~sees]).all()
+                g, ref, bound = g[~sees], ref[~sees], bound[~sees]
+            assert np.all(np.abs(g - ref) <= bound), (s, h, float(np.max(np.abs(g - ref) / bound)))
+            worst = max(worst, float(np.max(np.abs(g - ref) / bound)) if g.size else 0.0)
+    return worst
+
+
+@pytest.mark.parametrize("b,B,P,Hq,Hkv,dh", [
+    (1, 1, 0, 1, 1, 64), (1, 1, 0, 4, 2, 128), (1, 1, 300, 32, 32, 128), (2, 3, 1, 4, 4, 64), (1, 16, 31, 4, 4, 128),
+    (1, 16, 32, 4, 4, 128), (1, 17, 33, 4, 4, 64), (3, 32, 512, 4, 4, 128), (2, 37, 45, 14, 2, 128), (1, 64, 129, 28, 4, 128),
+    (1, 100, 77, 6, 3, 64), (1, 256, 40, 4, 1, 128), (1, 255, 3, 3, 3, 64), (2, 33, 1000, 7, 1, 128)])
+def test_attention(b, B, P, Hq, Hkv, dh):
+    announce("attention mx", b, B, P, Hq, Hkv, dh)
+    attention_case(b, B, P, Hq, Hkv, dh)
+
+
+@pytest.mark.parametrize("flags", [O.F_XSELF_SHADOW, O.F_MKEYS_SHADOW, O.F_C_BIDIR, O.F_ORDER_L2R,
+                                   O.F_XSELF_SHADOW | O.F_ORDER_L2R | O.F_MKEYS_SHADOW])
+def test_attention_mask_flags(flags):
+    announce("attention mx flags", flags)
+    attention_case(2, 41, 70, 4, 2, 64, flags=flags, seed=3)
+    attention_case(1, 70, 13, 2, 2, 128, flags=flags, seed=4)
+
+
+@pytest.mark.parametrize("b,B,P,Hq,Hkv,dh,lens", [
+    (4, 16, 100, 4, 2, 128, [0, 100, 1, 55]), (3, 33, 640, 2, 2, 64, [-5, 700, 320]), (5, 1, 64, 8, 1, 128, [0, 1, 31, 32, 64]),
+    (2, 64, 3000, 4, 4, 128, [17, 2999])])
+def test_attention_prefix_lengths(b, B, P, Hq, Hkv, dh, lens):
+    announce("attention mx prefix lengths", b, B, P, lens)
+    attention_case(b, B, P, Hq, Hkv, dh, lens=lens, cap_extra=32)
+
+
+@pytest.mark.parametrize("B,P,Hq,Hkv,dh", [(8, 6000, 4, 1, 128), (32, 20000, 7, 1, 128), (4, 9000, 2, 2, 64)])
+def test_attention_long(B, P, Hq, Hkv, dh):
+    announce("attention mx long", B, P, Hq, Hkv, dh)
+    attention_case(1, B, P, Hq, Hkv, dh, seed=5)
+
+
+def test_attention_peaked():
+    """Scores far apart: the running maximum moves, and most probabilities vanish."""
+    announce("attention mx peaked")
+    attention_case(1, 20, 500, 4, 2, 128, seed=6, qstd=8.0)
+
+
+@pytest.mark.parametrize("j", [0, 5, 12 + 5])
+def test_attention_nan_block_reaches_only_rows_that_see_it(j):
+    """Key j of the block (x below 12, then its shadow) with NaN blocks in K and V of one KV head."""
+    announce("attention mx nan", j)
+    attention_case(1, 12, 40, 4, 2, 128, seed=7, nan_key=(1, j, 3))
+    attention_case(2, 12, 27, 2, 2, 64, seed=8, nan_key=(0, j, 1))
+
+
+def test_attention_nan_value_block():
+    """A NaN block in V alone makes its 32 dims NaN in the rows that see the key, and nothing else."""
+    announce("attention mx nan value")
+    B, P, H, dh = 10, 35, 2, 128
+    rng = np.random.default_rng(9)
+    cap = 64
+    code, scale = R.quantize(rng.standard_normal((2, 1, H, cap, dh)), R.FP4)
+    scale[1, 0, 1, P + 4, 2] = 255
+    vc, vs = R.grouped(R.pack(code[1], R.FP4), scale[1])
+    state, conf = block(1, B, 1)
+    q = torch.from_numpy(rng.standard_normal((1, 2 * B, H, dh))).bfloat16().cuda()
+    out = torch.empty_like(q)
+    room = torch.empty(dard.dard_attention_mx_workspace_bytes(1, B, H, H, dh, P), dtype=torch.uint8, device="cuda")
+    dard.dard_masked_attention_mx(q, [dev(R.pack(code[0], R.FP4)), dev(scale[0]), dev(vc), dev(vs)], P, dev(state), dev(conf),
+                                  dh ** -0.5, 0, out, ws=room)
+    nan = torch.isnan(out).cpu().numpy()[0]
+    want = np.zeros_like(nan)
+    want[visible(state[0], conf[0], P, 0)[:, P + 4], 1, 64:96] = True
+    assert np.array_equal(nan, want)
+
+
+def test_attention_cache_past_4_gib():
+    """Offsets past 32 bits: the codes of K alone take 4.5 GiB."""
+    announce("attention mx long cache")
+    b, Hkv, dh, B, P = 9, 4, 128, 4, 2 * 1024 * 1024 - 2 * 4
+    cap = P + 2 * B
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GB of free device memory")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    kc = torch.randint(0, 256, (b, Hkv, cap, dh // 2), dtype=torch.uint8, generator=g, device="cuda")
+    vc = torch.randint(0, 256, (b, Hkv, cap // 8, dh // 4, 8, 2), dtype=torch.uint8, generator=g, device="cuda")
+    ks = torch.full((b, Hkv, cap, dh // 32), 126, dtype=torch.uint8, device="cuda")
+    vs = torch.full((b, Hkv, cap // 8, dh // 32, 8), 126, dtype=torch.uint8, device="cuda")
+    lens = torch.tensor([0] * (b - 1) + [P], dtype=torch.int32, device="cuda")
+    # the last sequence's last prefix keys must decide: they get a large scale in the last head
+    ks[-1, -1, P - 3:P] = 131
+    state, conf = block(b, B, 2)
+    q = torch.randn(b, 2 * B, Hkv, dh, generator=g, device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    room = torch.empty(dard.dard_attention_mx_workspace_bytes(b, B, Hkv, Hkv, dh, P), dtype=torch.uint8, device="cuda")
+    dard.dard_masked_attention_mx(q, (kc, ks, vc, vs), P, dev(state), dev(conf), dh ** -0.5, 0, out, ws=room, prefix=lens)
+    seen = torch.from_numpy(visible(state[-1], conf[-1], 0, 0)).cuda()
+    table = torch.from_numpy(R.F4).cuda().float()
+    s, h = b - 1, Hkv - 1
+
+    def vals(c):
+        return torch.stack([table[(c & 15).long()], table[(c >> 4).long()]], -1).flatten(-2)
+
+    m = torch.full((2 * B,), -float("inf"), dtype=torch.float64, device="cuda")
+    l, o, mass = torch.zeros_like(m), torch.zeros(2 * B, dh, dtype=torch.float64, device="cuda"), 0.0
+    qf = q[s, :, h].double()
+    step = 1 << 17
+    for at in range(0, cap, step):
+        n = min(step, cap - at)
+        k = vals(kc[s, h, at:at + n]).double() * torch.exp2(ks[s, h, at:at + n, :1].double() - 127)
+        v = vals(vc[s, h, at // 8:(at + n) // 8].permute(0, 2, 1, 3).reshape(n, dh // 2)).double() / 2
+        sc = qf @ k.T * dh ** -0.5
+        if at + n > P:
+            sc[:, P - at:] = sc[:, P - at:].masked_fill(~seen, -float("inf"))
+        mn = torch.maximum(m, sc.amax(-1))
+        p = torch.exp(sc - mn[:, None])
+        f = torch.exp(m - mn)
+        l, o, mass = l * f + p.sum(-1), o * f[:, None] + p @ v, (mass * f[:, None] if at else 0.0) + p @ v.abs()
+        m = mn
+    err = (out[s, :, h].double() - o / l[:, None]).abs()
+    assert bool((err <= (2.0 ** -7 + 2.0 ** -12) * mass / l[:, None]).all())
+
+
+# ------------------------------------------------------------------ the operators together
+def test_layer_half_captured_and_replayed():
+    """Norm, QKV product, cache write, attention, quantised output, O product and the next norm, as a
+    serving loop runs them: eager, then captured into a graph and replayed on new inputs between
+    eager runs; every replay equals the eager result bit for bit.  The eager result of each stage
+    is checked against the plain form on the stage's own inputs."""
+    announce("mx chain")
+    b, B, P, Hq, Hkv, dh = 2, 16, 45, 4, 2, 64
+    d, n = Hq * dh, (Hq + 2 * Hkv) * dh
+    rows = b * 2 * B
+    g = torch.Generator(device="cuda").manual_seed(3)
+    u8 = lambda *s: torch.empty(*s, dtype=torch.uint8, device="cuda")   # noqa: E731
+    weights = []
+    for N, K in ((n, d), (d, d)):
+        w = torch.randn(N, K, generator=g, device="cuda") * K ** -0.5
+        wc, ws, wp = u8(N, K // 2), u8(N, K // 32), u8(dard.dard_packed_mx_bytes(N, K))
+        dard.dard_quantize_mx(w, dard.MX_FP4, wc, ws)
+        dard.dard_pack_matrix_mx(wc, ws, wp)
+        weights.append((wp, R.values(R.unpack(wc.cpu().numpy(), R.FP4), ws.cpu().numpy(), R.FP4)))
+    gain = (1 + 0.1 * torch.randn(d, generator=g, device="cuda")).bfloat16()
+    cap = 96
+    cache = [dev(t) for t in empty_cache(b, Hkv, cap, dh, 0)]
+    pre = torch.randn(2, b, P, Hkv, dh, generator=g, device="cuda").bfloat16()
+    dard.dard_kv_write_mx(pre[0], pre[1], cache, 0)
+    state, conf = (dev(t) for t in block(b, B, 4))
+    h = torch.empty(rows, d, device="cuda")
+    delta = torch.zeros(rows, d, device="cuda")
+    xc, xs, ac, asc = u8(rows, d), u8(rows, d // 32), u8(rows, d), u8(rows, d // 32)
+    oc, osc = u8(rows, d), u8(rows, d // 32)
+    qkv = torch.empty(b, 2 * B, Hq + 2 * Hkv, dh, dtype=torch.bfloat16, device="cuda")
+    q = torch.empty(b, 2 * B, Hq, dh, dtype=torch.bfloat16, device="cuda")
+    att, y = torch.empty_like(q), torch.empty(rows, d, device="cuda")
+    room = u8(max(16, dard.dard_attention_mx_workspace_bytes(b, B, Hq, Hkv, dh, P),
+                  dard.dard_linear_mx_workspace_bytes(dard.MX_FP8, rows, n, d)))
+
+    def layer():
+        dard.dard_resid_norm_mx(h, gain, 1e-5, dard.MX_FP8, xc, xs, delta=delta)
+        dard.dard_linear_mx(dard.MX_FP8, xc, xs, weights[0][0], qkv.view(rows, n), ws=room)
+        q.copy_(qkv[:, :, :Hq])
+        dard.dard_kv_write_mx(qkv[:, :, Hq:Hq + Hkv], qkv[:, :, Hq + Hkv:], cache, P)
+        dard.dard_masked_attention_mx(q, cache, P, state, conf, dh ** -0.5, 0, att, ws=room)
+        dard.dard_quantize_mx(att.view(rows, d), dard.MX_FP8, ac, asc)
+        dard.dard_linear_mx(dard.MX_FP8, ac, asc, weights[1][0], y, ws=room)
+        dard.dard_resid_norm_mx(h, gain, 1e-5, dard.MX_FP8, oc, osc, delta=y)
+
+    inputs = [torch.randn(rows, d, generator=g, device="cuda") for _ in range(3)]
+    eager = []
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for x in inputs:
+            h.copy_(x)
+            layer()
+            eager.append([t.clone() for t in (qkv, att, y, h, oc, osc, *cache)])
+            # (the residual stream of the next input is copied over: nothing carries on)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            layer()
+        for i in (2, 0, 1, 1):
+            h.copy_(inputs[i])
+            graph.replay()
+            torch.cuda.synchronize()
+            for got, ref in zip((qkv, att, y, h, oc, osc, *cache), eager[i]):
+                assert torch.equal(got, ref), i
+            h.copy_(inputs[0])
+            layer()   # eager work between the replays
+            torch.cuda.synchronize()
+            for got, ref in zip((qkv, att, y, h, oc, osc, *cache), eager[0]):
+                assert torch.equal(got, ref)
+    torch.cuda.current_stream().wait_stream(side)
+    # the stages of input 1, each on what the one before it gave
+    qkv_, att_, y_, h_ = (t.double().cpu().numpy() for t in eager[1][:4])
+    _, yn = R.norm(inputs[1].cpu().numpy(), None, gain.float().cpu().numpy(), 1e-5)
+    x = R.values(*R.quantize(yn, R.FP8), R.FP8)
+    ref = x @ weights[0][1].T
+    bound = R.product_bound(x, weights[0][1], scaled=True)
+    assert np.all(np.abs(qkv_.reshape(rows, n) - ref) <= bound + (np.abs(ref) + bound) * 2.0 ** -8)
+    a = R.values(*R.quantize(att_.reshape(rows, d), R.FP8), R.FP8)
+    ref = a @ weights[1][1].T
+    assert np.all(np.abs(y_ - ref) <= R.product_bound(a, weights[1][1], scaled=True))
+    kall = [np.concatenate([pre[i].double().cpu().numpy(), qkv_[:, :, Hq + i * Hkv:Hq + (i + 1) * Hkv]], 1) for i in (0, 1)]
+    k, v = (R.values(*R.quantize(t, R.FP4), R.FP4) for t in kall)
+    for s in range(b):
+        seen = visible(state[s].cpu().numpy(), conf[s].cpu().numpy(), P, 0)
+        for hh in range(Hq):
+            ref, bound = attend(qkv_[s, :, hh], k[s, :, hh // 2], v[s, :, hh // 2], seen, dh ** -0.5)
+            assert np.all(np.abs(att_[s, :, hh] - ref) <= bound)
+    want, yn = R.norm(inputs[1].cpu().numpy(), y_.astype(np.float32), gain.float().cpu().numpy(), 1e-5)
+    assert np.array_equal(h_.astype(np.float32), want)
+    c, s8 = R.quantize(yn, R.FP8)
+    assert np.array_equal(eager[1][4].cpu().numpy(), c) and np.array_equal(eager[1][5].cpu().numpy(), s8)
