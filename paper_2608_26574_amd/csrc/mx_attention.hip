@@ -33,96 +33,261 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFloor = -1e30f;   // running-max floor (log2 units): exp2 of anything below it is 0
+constexpr float kBig = 256.f;      // a lane's probability sum over a tile that moves the running max
 constexpr int kTileKeys = 32;
 constexpr int kVisWords = 2 * kMaxBlock / 32 + 2;   // 32-bit words of a row's visibility, padded
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Two floats to bf16 (the hardware's conversion: nearest even, NaN stays NaN).
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    return (uint32_t)f2bf(lo) | ((uint32_t)f2bf(hi) << 16);
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, bf16x2));
 }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __builtin_bit_cast(bf16x8, make_uint4(a, b, c, d));
 }
 
-// Codes and scales of one key tile as a lane loads them.
-template <int DH> struct Raw {
-    uint4 k[DH / 64];     // this lane's half key
-    uint32_t ks;          // its scales (one byte per 32 dims)
-    uint4 v[2];           // 8 keys of this lane's dims, steps m = 0, 1
-    uint2 vs[2];          // their scales
+// Codes and scales of one key tile as a lane reads them from LDS (vector types:
+// reads of the uint4 struct lose the type information without which the compiler
+// makes them wait for every copy in flight).
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+template <int DH> struct RawK {
+    uintx4 c[DH / 64];    // this lane's half key
+    uint32_t s;           // its scales (one byte per 32 dims)
+};
+struct RawV {
+    uintx4 c[2];          // 8 keys of this lane's dims, steps m = 0, 1
+    uintx2 s[2];          // their scales
 };
 
-template <int DH>
-__device__ __forceinline__ Raw<DH> load_tile(const MxAttnArgs& a, size_t row0, int k0, int lane) {
-    const int lr = lane & 31, eta = lane >> 5;
-    Raw<DH> t;
-    const size_t key = row0 + k0 + ((lr & ~12) | ((lr & 4) << 1) | ((lr & 8) >> 1));
-    const uint4* kp = reinterpret_cast<const uint4*>(a.kc + key * (DH / 2) + eta * (DH / 4));
+// A wave's ring of key tiles in LDS.  Copies run kDepth tiles ahead straight from
+// memory to LDS (no registers), so a wave keeps enough loads in flight to cover the
+// memory's latency on its own; the ring is the wave's alone, so its waits are counts of its
+// own copies.  A slot holds every lane's operands in lane order (reads of 16
+// bytes are consecutive over the lanes): K codes [DH/64][64][16], V codes
+// [DH/64][64][16], then the DH bytes of K scales and the DH of V scales.
+template <int DH> struct Slot {
+    static constexpr int kV = DH * 16, kKs = 2 * kV, kVs = kKs + DH, kBytes = kVs + DH;
+    static constexpr int kCopies = 2 * (DH / 64) + 2;
+};
+
+__device__ __forceinline__ void copy16_lds(__amdgpu_buffer_rsrc_t r, char* dst, int voff) {
+#if __HIP_DEVICE_COMPILE__   // (the host pass does not know the builtin)
+    typedef __attribute__((address_space(3))) void* lds_ptr;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, voff, 0, 0, 0);
+#endif
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint8_t* p) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, (short)0, -1, 0x00020000);
+}
+
+// Cache of one sequence and KV head, and this lane's byte offsets in a tile.
+template <int DH> struct Tiles {
+    const uint8_t *kc, *ks, *vc, *vs;   // at key 0
+    int ko, vo, vs16;
+    bool scales;                        // lanes that copy the tile's DH scale bytes
+    __device__ __forceinline__ Tiles(const MxAttnArgs& a, size_t row0, int lane) {
+        kc = a.kc + row0 * (DH / 2);
+        ks = a.ks + row0 * (DH / 32);
+        vc = a.vc + row0 * (DH / 2);
+        vs = a.vs + row0 * (DH / 32);
+        const int lr = lane & 31, eta = lane >> 5;
+        ko = ((lr & ~12) | ((lr & 4) << 1) | ((lr & 8) >> 1)) * (DH / 2) + eta * (DH / 4);
+        vo = DH == 128 ? (eta * 32 + lr) * 16 : lane * 16;
+        vs16 = lane * 16;
+        scales = lane < DH / 16;
+    }
+    __device__ __forceinline__ void copy(int t, char* slot) const {
+        const __amdgpu_buffer_rsrc_t k = rsrc(kc + (size_t)t * (16 * DH)), v = rsrc(vc + (size_t)t * (16 * DH));
 #pragma unroll
-    for (int i = 0; i < DH / 64; ++i) t.k[i] = kp[i];
-    if constexpr (DH == 128) t.ks = reinterpret_cast<const uint16_t*>(a.ks)[key * 2 + eta];
-    else t.ks = a.ks[key * 2 + eta];
+        for (int i = 0; i < DH / 64; ++i) copy16_lds(k, slot + i * 1024, ko + 16 * i);
+#pragma unroll
+        for (int i = 0; i < DH / 64; ++i) copy16_lds(v, slot + Slot<DH>::kV + i * 1024, vo + 1024 * i);
+        if (scales) {
+            copy16_lds(rsrc(ks + (size_t)t * DH), slot + Slot<DH>::kKs, vs16);
+            copy16_lds(rsrc(vs + (size_t)t * DH), slot + Slot<DH>::kVs, vs16);
+        }
+    }
+};
+
+template <int DH> __device__ __forceinline__ RawK<DH> read_k(const char* slot, int lane) {
+    RawK<DH> t;
+    const int lr = lane & 31, eta = lane >> 5, key = (lr & ~12) | ((lr & 4) << 1) | ((lr & 8) >> 1);
+#pragma unroll
+    for (int i = 0; i < DH / 64; ++i) t.c[i] = *reinterpret_cast<const uintx4*>(slot + i * 1024 + lane * 16);
+    if constexpr (DH == 128) t.s = *reinterpret_cast<const uint16_t*>(slot + Slot<DH>::kKs + key * 4 + 2 * eta);
+    else t.s = *reinterpret_cast<const uint8_t*>(slot + Slot<DH>::kKs + key * 2 + eta);
+    return t;
+}
+template <int DH> __device__ __forceinline__ RawV read_v(const char* slot, int lane) {
+    RawV t;
+    const int lr = lane & 31, eta = lane >> 5;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        const size_t grp = ((row0 + k0) >> 3) + 2 * m + eta;
-        const int quad = DH == 128 ? lr : lr >> 1, blk = DH == 128 ? lr >> 3 : lr >> 4;
-        t.v[m] = *reinterpret_cast<const uint4*>(a.vc + (grp * (DH / 4) + quad) * 16);
-        t.vs[m] = *reinterpret_cast<const uint2*>(a.vs + (grp * (DH / 32) + blk) * 8);
+        const int grp = 2 * m + eta, blk = DH == 128 ? lr >> 3 : lr >> 4;
+        t.c[m] = *reinterpret_cast<const uintx4*>(slot + Slot<DH>::kV + (DH == 128 ? m * 1024 + lane * 16 : (grp * 16 + (lr >> 1)) * 16));
+        t.s[m] = *reinterpret_cast<const uintx2*>(slot + Slot<DH>::kVs + (grp * (DH / 32) + blk) * 8);
     }
     return t;
 }
 
-// Does the row (position i, shadow) see key idx of the block (x keys, then s keys)?
-__device__ __forceinline__ bool sees(const uint8_t* st, const float* cf, int i, bool shadow, int idx, int B,
-                                     uint32_t flags) {
-    if (idx >= 2 * B) return false;
-    const int j = idx < B ? idx : idx - B;
-    return take_x(st[i], st[j], cf[i], cf[j], i, j, shadow, flags) == (idx < B);
+// Byte i of w as the scale of a conversion.  Those read a float's exponent
+// field alone (checked with every other bit set and clear), so one shift does.
+template <int I> __device__ __forceinline__ float scale_at(uint32_t w) {
+    return __uint_as_float(I < 3 ? w << (23 - 8 * I) : w >> 1);
+}
+
+// Bits [start, start + 64) of a bit string of kBlockWords words, zero outside.
+__device__ __forceinline__ uint64_t bits_at(const uint64_t* x, int start) {
+    if (start <= -64 || start >= 64 * kBlockWords) return 0ull;
+    if (start < 0) return x[0] << -start;
+    const int q = start >> 6, sh = start & 63;
+    uint64_t v = x[q] >> sh;
+    if (sh && q + 1 < kBlockWords) v |= x[q + 1] << (64 - sh);
+    return v;
+}
+
+// Position of workgroup `id` of `total` when the eight XCDs, which take
+// workgroups in turn, each get one contiguous run.
+__device__ __forceinline__ int xcd_run(int id, int total) {
+    const int x = id & 7, q = total >> 3, r = total & 7;
+    return x * q + min(x, r) + (id >> 3);
+}
+
+// S^T = K Q^T of one tile.
+template <int DH, int JT>
+__device__ __forceinline__ void scores(const RawK<DH>& k, const bf16x8 (&q)[JT][DH / 16], floatx16 (&st)[JT]) {
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) st[jt] = floatx16{};
+    const float f[2] = {scale_at<0>(k.s), scale_at<1>(k.s)};
+#pragma unroll
+    for (int j = 0; j < DH / 16; ++j) {
+        const uint32_t x = k.c[j / 4][j & 3];
+        const bf16x8 kf = as_bf16x8(fp4x2_to_bf16x2<0>(x, f[j / 4]), fp4x2_to_bf16x2<1>(x, f[j / 4]),
+                                    fp4x2_to_bf16x2<2>(x, f[j / 4]), fp4x2_to_bf16x2<3>(x, f[j / 4]));
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt) st[jt] = mfma32x32x16(kf, q[jt][j], st[jt]);
+    }
+}
+
+// Probabilities of one tile against the running maximum m (log2 units, c =
+// log2 units per score), which may lag the true one: a lane whose sum of them
+// exceeds kBig (always on a row's first visible tile, and whenever a score is
+// more than 8 above m) has the tile's maximum taken, the accumulators rescaled
+// and the probabilities formed again, so other tiles need no maximum.
+template <int JT, int NT>
+__device__ __forceinline__ void probabilities(const floatx16 (&st)[JT], float c, float (&m)[JT], float (&l)[JT],
+                                              floatx16 (&o)[JT][NT], uint32_t (&p)[JT][8]) {
+    float sum[JT];
+    auto form = [&](int jt) __attribute__((always_inline)) {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p0 = exp2_fast(fmaf(st[jt][2 * e], c, -m[jt])), p1 = exp2_fast(fmaf(st[jt][2 * e + 1], c, -m[jt]));
+            a += p0;
+            b += p1;
+            p[jt][e] = pack_bf16(p0, p1);
+        }
+        sum[jt] = a + b;
+    };
+    bool big = false;
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) {
+        form(jt);
+        big |= sum[jt] > kBig;
+    }
+    if (__builtin_expect(__any(big), 0)) {
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt) {
+            float top = st[jt][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = fmaxf(top, st[jt][e]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float mn = fmaxf(m[jt], top * c);
+            const float al = exp2_fast(m[jt] - mn);
+            m[jt] = mn;
+            l[jt] *= al;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[jt][t][e] *= al;
+            form(jt);
+        }
+    }
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) l[jt] += sum[jt];
+}
+
+// O^T += V^T P^T of one tile.
+template <int DH, int JT>
+__device__ __forceinline__ void add_values(const RawV& v, const uint32_t (&p)[JT][8], int lr, floatx16 (&o)[JT][DH / 32]) {
+    constexpr int NT = DH / 32;
+#pragma unroll
+    for (int mm = 0; mm < 2; ++mm) {
+        uint32_t vf[NT][4];
+        const float f[8] = {scale_at<0>(v.s[mm].x), scale_at<1>(v.s[mm].x), scale_at<2>(v.s[mm].x), scale_at<3>(v.s[mm].x),
+                            scale_at<0>(v.s[mm].y), scale_at<1>(v.s[mm].y), scale_at<2>(v.s[mm].y), scale_at<3>(v.s[mm].y)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {   // keys 2 i, 2 i + 1
+            if constexpr (DH == 128) {
+                const uint32_t a0 = fp4x2_to_bf16x2<0>(v.c[mm][i], f[2 * i]), a1 = fp4x2_to_bf16x2<1>(v.c[mm][i], f[2 * i]);
+                const uint32_t b0 = fp4x2_to_bf16x2<2>(v.c[mm][i], f[2 * i + 1]), b1 = fp4x2_to_bf16x2<3>(v.c[mm][i], f[2 * i + 1]);
+                vf[0][i] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+                vf[1][i] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+                vf[2][i] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+                vf[3][i] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+            } else {
+                const uint32_t x = v.c[mm][i] >> (8 * (lr & 1));   // this lane's two dims of the four
+                const uint32_t a0 = fp4x2_to_bf16x2<0>(x, f[2 * i]), b0 = fp4x2_to_bf16x2<2>(x, f[2 * i + 1]);
+                vf[0][i] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+                vf[1][i] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt)
+                o[jt][t] = mfma32x32x16(as_bf16x8(vf[t][0], vf[t][1], vf[t][2], vf[t][3]),
+                                        as_bf16x8(p[jt][4 * mm], p[jt][4 * mm + 1], p[jt][4 * mm + 2], p[jt][4 * mm + 3]),
+                                        o[jt][t]);
+    }
 }
 
 template <int DH, int JT>
-__global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3 - JT)))
+void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
     constexpr int NJ = DH / 16, NT = DH / 32;
-    __shared__ __attribute__((aligned(16))) float smem[4 * NT * 4 * 64 * 4];   // O of one row tile of the four waves
-    __shared__ float ml[4][JT][2][32];
-    __shared__ uint32_t vis[32 * JT][kVisWords];
-    __shared__ uint8_t sst[kMaxBlock];
-    __shared__ float scf[kMaxBlock];
+    constexpr int kDepth = JT == 2 ? 7 : 4;            // tiles in flight per wave (one and two workgroups a CU)
+    constexpr int kRing = kDepth * Slot<DH>::kBytes;
+    static_assert(kDepth * Slot<DH>::kCopies <= 63, "vmcnt range");
+    static_assert(4 * kRing >= 4 * NT * 4 * 64 * 16, "the merge of the waves fits the rings");
+    // One array (several would carry alias information by which the compiler makes every LDS read
+    // wait for every copy in flight): the rings, which at the end hold O of one row tile of the four
+    // waves; the waves' maxima and sums; the rows' take-x words and their complements; the
+    // rows' visibility strings.
+    constexpr int kMl = 4 * kRing, kXs = kMl + 4 * JT * 64 * 4, kVis = kXs + 32 * JT * 2 * kBlockWords * 8;
+    __shared__ __attribute__((aligned(16))) char smem[kVis + 32 * JT * kVisWords * 4];
+    float* const ml = reinterpret_cast<float*>(smem + kMl);
+    uint64_t* const xs = reinterpret_cast<uint64_t*>(smem + kXs);
+    uint64_t* const vis = reinterpret_cast<uint64_t*>(smem + kVis);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 31, eta = lane >> 5;
-    const int rt = blockIdx.x % rowtiles, kvh = blockIdx.x / rowtiles % a.Hkv, s = blockIdx.x / rowtiles / a.Hkv;
+    const int nsplit = gridDim.y;
+    int id = xcd_run(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * nsplit);
+    const int rt = id % rowtiles;
+    id /= rowtiles;
+    const int split = id % nsplit;
+    id /= nsplit;
+    const int kvh = id % a.Hkv, s = id / a.Hkv;
     const int R = 2 * a.B, GQ = a.Hq / a.Hkv, nrows = GQ * R;
     int P = a.P;
     if (a.prefix) P = min(max(__builtin_amdgcn_readfirstlane(a.prefix[s]), 0), a.P);
     const int nkeys = P + R, ntiles = (nkeys + kTileKeys - 1) / kTileKeys;
-    const int t0 = blockIdx.y * tps, t1 = min(ntiles, t0 + tps);
-
-    // visibility strings of the workgroup's rows, where its keys reach the block
-    if (t1 * kTileKeys > P && t0 < t1) {
-        for (int i = threadIdx.x; i < a.B; i += 256) {
-            sst[i] = a.state[(size_t)s * a.B + i];
-            scf[i] = a.conf[(size_t)s * a.B + i];
-        }
-        __syncthreads();
-        const int words = (R + 31) / 32;
-        for (int i = threadIdx.x; i < 32 * JT * kVisWords; i += 256) {
-            const int row = i / kVisWords, w = i % kVisWords;
-            uint32_t bits = 0;
-            const int rho = rt * 32 * JT + row;
-            if (w < words && rho < nrows) {
-                const int r = rho % R;
-                const bool shadow = r >= a.B;
-                const int pos = shadow ? r - a.B : r;
-                for (int b = 0; b < 32; ++b)
-                    bits |= (uint32_t)sees(sst, scf, pos, shadow, 32 * w + b, a.B, a.flags) << b;
-            }
-            vis[row][w] = bits;
-        }
-    }
-    __syncthreads();
+    const int t0 = split * tps, t1 = min(ntiles, t0 + tps);
 
     // this lane's query rows: dims of the half eta
     bf16x8 q[JT][NJ];
@@ -133,6 +298,78 @@ __global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles
 #pragma unroll
         for (int j = 0; j < NJ; ++j) q[jt][j] = ld_bf16x8(qp + 8 * j);
     }
+    // states and confidences: of a row of the tile, and of a block position of word `wave`
+    const bool block = t1 * kTileKeys > P && t0 < t1;   // (the same for the workgroup)
+    const int row = rt * 32 * JT + (JT == 2 ? lane : lr), r = min(row, nrows - 1) % R;
+    const bool shadow = r >= a.B;
+    const int pos = shadow ? r - a.B : r, wpos = 64 * wave + lane;
+    int si = 0, sj = -1;
+    float ci = 0.f, cj = 0.f;
+    if (block) {
+        const uint8_t* state = a.state + (size_t)s * a.B;
+        const float* conf = a.conf + (size_t)s * a.B;
+        si = state[pos];
+        ci = conf[pos];
+        if (wpos < a.B) {
+            sj = state[wpos];
+            cj = conf[wpos];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);   // (these loads before the rings' copies: waits are in order)
+    const size_t row0 = ((size_t)s * a.Hkv + kvh) * a.cap;
+    // this wave's tiles: t0 + wave + 4 i for i < n, the first `full` of them seen whole by
+    // every row.  Tile i sits in ring slot i % kDepth; copies past the last repeat it, so that the
+    // number in flight is always the same.
+    const Tiles<DH> tiles(a, row0, lane);
+    char* ring = smem + wave * kRing;
+    const int first = t0 + wave, n = max(0, (t1 - first + 3) >> 2);
+    const int full = max(0, (min(t1, P / kTileKeys) - first + 3) >> 2);
+    int at = 0;            // ring slot of tile i
+    auto next_slot = [&](int x) { return x + 1 == kDepth ? 0 : x + 1; };
+    if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) tiles.copy(first + 4 * min(i, n - 1), ring + i * Slot<DH>::kBytes);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // Visibility strings of the workgroup's rows, where its keys reach the block: wave w forms the
+    // 64 positions from 64 w on of every row (a lane per row).  The rules are those of take_x:
+    // ballots give the U and C sets, a candidate row compares its confidence with every candidate's.
+    if (block) {
+        const uint64_t U = __ballot(sj == DARD_STATE_U), C = __ballot(sj == DARD_STATE_C);
+        const uint64_t in = block_word_mask(a.B, wave), self = (pos >> 6) == wave ? 1ull << (pos & 63) : 0ull;
+        uint64_t better = C;
+        if (a.flags & DARD_F_ORDER_L2R) {
+            const int upto = pos - 64 * wave + 1;   // positions of this word that are <= pos
+            better &= upto >= 64 ? ~0ull : (upto <= 0 ? 0ull : (1ull << upto) - 1);
+        } else if (!(a.flags & DARD_F_C_BIDIR)) {
+            better = 0ull;
+            for (uint64_t left = C; left; left &= left - 1) {
+                const int j = __builtin_ctzll(left);
+                const float x = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(cj), j));
+                better |= ci <= x ? 1ull << j : 0ull;
+            }
+        }
+        uint64_t x;
+        if (si == DARD_STATE_U) x = (shadow || (a.flags & DARD_F_XSELF_SHADOW)) ? U & ~self : U;
+        else if (si == DARD_STATE_C) x = shadow ? (U | better) & ~self : U | better;
+        else if (shadow) x = U;
+        else x = (a.flags & DARD_F_MKEYS_SHADOW) ? U | C | self : in;
+        if (JT == 2 || eta == 0) {
+            xs[(JT == 2 ? lane : lr) * 2 * kBlockWords + wave] = x;
+            xs[(JT == 2 ? lane : lr) * 2 * kBlockWords + kBlockWords + wave] = ~x & in;
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
+        wg_barrier();
+        // bit j of a row's string: key j of the block, x keys (bits of x), then s keys (the others)
+        for (int i = threadIdx.x; i < 32 * JT * kVisWords / 2; i += 256) {
+            const uint64_t* w = xs + i / (kVisWords / 2) * 2 * kBlockWords;
+            const int start = 64 * (i % (kVisWords / 2));
+            vis[i] = bits_at(w, start) | bits_at(w + kBlockWords, start - a.B);
+        }
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
+        wg_barrier();
+    }
+
     const float c = a.scale * kLog2e;
     floatx16 o[JT][NT];
     float m[JT], l[JT];
@@ -143,146 +380,109 @@ __global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[jt][t] = floatx16{};
     }
-    const size_t row0 = ((size_t)s * a.Hkv + kvh) * a.cap;
 
-    for (int t = t0 + wave; t < t1; t += 4) {
-        const int k0 = t * kTileKeys;
-        Raw<DH> raw = load_tile<DH>(a, row0, k0, lane);
-        // scores
-        floatx16 st[JT];
-#pragma unroll
-        for (int jt = 0; jt < JT; ++jt) st[jt] = floatx16{};
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const uint4 w = raw.k[j / 4];
-            const uint32_t x = (j & 3) == 0 ? w.x : (j & 3) == 1 ? w.y : (j & 3) == 2 ? w.z : w.w;
-            const float f = mx_scale_f((raw.ks >> (8 * (j / 4))) & 255u);
-            const bf16x8 kf = as_bf16x8(fp4x2_to_bf16x2<0>(x, f), fp4x2_to_bf16x2<1>(x, f), fp4x2_to_bf16x2<2>(x, f),
-                                        fp4x2_to_bf16x2<3>(x, f));
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) st[jt] = mfma32x32x16(kf, q[jt][j], st[jt]);
-        }
-        // visibility: element 8 m + e of a lane is key k0 + 16 m + 8 eta + e
-        const bool edge = k0 + kTileKeys > P;
-        uint32_t seen[JT];
-        uint32_t bad[NT];   // keys whose V block of 32 dims reads as NaN (edge tiles only)
-        if (edge) {
-            const int j0 = k0 - P;
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-                const uint32_t* v = vis[32 * jt + lr];
-                uint32_t bits;
-                if (j0 < 0) {
-                    bits = (v[0] << -j0) | ((1u << -j0) - 1u);   // (-j0 < 32)
-                } else {
-                    const int w = j0 >> 5, sh = j0 & 31;
-                    bits = sh ? (v[w] >> sh) | (v[w + 1] << (32 - sh)) : v[w];
-                }
-                seen[jt] = bits;
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    st[jt][e] = (bits >> (16 * (e / 8) + 8 * eta + e % 8)) & 1u ? st[jt][e] : -INFINITY;
-            }
-            // a V block with a NaN scale would reach rows that do not see its key (0 * NaN):
-            // read it as zeros and note the key
-            uint32_t mine = 0;
-#pragma unroll
-            for (int mm = 0; mm < 2; ++mm) {
-                uint32_t* sc = &raw.vs[mm].x;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t b = (sc[e / 4] >> (8 * (e & 3))) & 255u;
-                    if (b == 255u) {
-                        mine |= 1u << (16 * mm + 8 * eta + e);
-                        sc[e / 4] &= ~(255u << (8 * (e & 3)));
-                    }
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < NT; ++b) {
-                const int src = b * (32 / NT);
-                bad[b] = (uint32_t)__shfl((int)mine, src, 64) | (uint32_t)__shfl((int)mine, src + 32, 64);
-            }
-        }
-        // softmax
-        uint32_t p[JT][8];
-#pragma unroll
-        for (int jt = 0; jt < JT; ++jt) {
-            float top = st[jt][0];
-#pragma unroll
-            for (int e = 1; e < 16; ++e) top = fmaxf(top, st[jt][e]);
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float mn = fmaxf(m[jt], top * c);
-            const float al = exp2_fast(m[jt] - mn);
-            m[jt] = mn;
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float p0 = exp2_fast(fmaf(st[jt][2 * e], c, -mn)), p1 = exp2_fast(fmaf(st[jt][2 * e + 1], c, -mn));
-                sum += p0 + p1;
-                p[jt][e] = pack_bf16(p0, p1);
-            }
-            l[jt] = l[jt] * al + sum;
-#pragma unroll
-            for (int t2 = 0; t2 < NT; ++t2)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[jt][t2][e] *= al;
-        }
-        // values
-#pragma unroll
-        for (int mm = 0; mm < 2; ++mm) {
-            uint32_t vf[NT][4];
-            const uint32_t rv[4] = {raw.v[mm].x, raw.v[mm].y, raw.v[mm].z, raw.v[mm].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {   // keys 2 i, 2 i + 1
-                const uint32_t sc = i < 2 ? raw.vs[mm].x : raw.vs[mm].y;
-                const float f0 = mx_scale_f((sc >> (16 * (i & 1))) & 255u), f1 = mx_scale_f((sc >> (16 * (i & 1) + 8)) & 255u);
-                if constexpr (DH == 128) {
-                    const uint32_t a0 = fp4x2_to_bf16x2<0>(rv[i], f0), a1 = fp4x2_to_bf16x2<1>(rv[i], f0);
-                    const uint32_t b0 = fp4x2_to_bf16x2<2>(rv[i], f1), b1 = fp4x2_to_bf16x2<3>(rv[i], f1);
-                    vf[0][i] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
-                    vf[1][i] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
-                    vf[2][i] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
-                    vf[3][i] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
-                } else {
-                    const uint32_t x = rv[i] >> (8 * (lr & 1));   // this lane's two dims of the four
-                    const uint32_t a0 = fp4x2_to_bf16x2<0>(x, f0), b0 = fp4x2_to_bf16x2<2>(x, f1);
-                    vf[0][i] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
-                    vf[1][i] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
-                }
-            }
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-                const bf16x8 pf = as_bf16x8(p[jt][4 * mm], p[jt][4 * mm + 1], p[jt][4 * mm + 2], p[jt][4 * mm + 3]);
-#pragma unroll
-                for (int t2 = 0; t2 < NT; ++t2)
-                    o[jt][t2] = mfma32x32x16(as_bf16x8(vf[t2][0], vf[t2][1], vf[t2][2], vf[t2][3]), pf, o[jt][t2]);
-            }
-        }
-        if (edge) {
-            // A row i = dim NT i + t: block of 32 dims (NT i + t) / 32 = i / (32 / NT), element e has i = 8 (e / 4) + ...
-            uint32_t any = 0;
-#pragma unroll
-            for (int b = 0; b < NT; ++b) any |= bad[b];
-            if (__any(any != 0)) {
-#pragma unroll
-                for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-                    for (int t2 = 0; t2 < NT; ++t2)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (seen[jt] & bad[8 * (e / 4) * NT / 32]) o[jt][t2][e] = __uint_as_float(0x7FC00000u);
-            }
+    auto refill = [&](int i) __attribute__((always_inline)) {   // tile i's slot, once its values are in registers
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
+        tiles.copy(first + 4 * min(i + kDepth, n - 1), ring + at * Slot<DH>::kBytes);
+        at = next_slot(at);
+    };
+    int i = 0;
+    if (full > 0) {
+        // while the probabilities of one tile are formed, the matrix cores run the scores of the next
+        floatx16 st[2][JT];
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((kDepth - 1) * Slot<DH>::kCopies));
+        __builtin_amdgcn_sched_barrier(0);
+        scores<DH, JT>(read_k<DH>(ring, lane), q, st[0]);
+        auto step = [&](const floatx16 (&cur)[JT], floatx16 (&nxt)[JT]) __attribute__((always_inline)) {
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm((kDepth - 2) * Slot<DH>::kCopies));   // tiles i and i + 1 are there
+            __builtin_amdgcn_sched_barrier(0);
+            const RawK<DH> k = read_k<DH>(ring + next_slot(at) * Slot<DH>::kBytes, lane);
+            const RawV v = read_v<DH>(ring + at * Slot<DH>::kBytes, lane);
+            uint32_t p[JT][8];
+            scores<DH, JT>(k, q, nxt);
+            probabilities<JT, NT>(cur, c, m, l, o, p);
+            add_values<DH, JT>(v, p, lr, o);
+            refill(i);
+            ++i;
+        };
+        while (true) {
+            step(st[0], st[1]);
+            if (i == full) break;
+            step(st[1], st[0]);
+            if (i == full) break;
         }
     }
+    // tiles at the prefix's end and in the block
+    for (; i < n; ++i) {
+        const int k0 = (first + 4 * i) * kTileKeys;
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((kDepth - 1) * Slot<DH>::kCopies));
+        __builtin_amdgcn_sched_barrier(0);
+        const RawK<DH> k = read_k<DH>(ring + at * Slot<DH>::kBytes, lane);
+        RawV v = read_v<DH>(ring + at * Slot<DH>::kBytes, lane);
+        floatx16 st[JT];
+        uint32_t p[JT][8], seen[JT];
+        scores<DH, JT>(k, q, st);
+        // element 8 m + e of a lane is key k0 + 16 m + 8 eta + e
+        const int j0 = k0 - P;
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt) {
+            const uint32_t* vw = reinterpret_cast<const uint32_t*>(vis) + (32 * jt + lr) * kVisWords;
+            uint32_t bits;
+            if (j0 < 0) {
+                bits = (vw[0] << -j0) | ((1u << -j0) - 1u);   // (-j0 < 32)
+            } else {
+                const int w = j0 >> 5, sh = j0 & 31;
+                bits = sh ? (vw[w] >> sh) | (vw[w + 1] << (32 - sh)) : vw[w];
+            }
+            seen[jt] = bits;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                st[jt][e] = (bits >> (16 * (e / 8) + 8 * eta + e % 8)) & 1u ? st[jt][e] : -INFINITY;
+        }
+        // a V block with a NaN scale would reach rows that do not see its key (0 * NaN):
+        // read it as zeros and note the key, per block of 32 dims
+        uint32_t mine = 0, bad[NT];
+#pragma unroll
+        for (int mm = 0; mm < 2; ++mm) {
+            uint32_t sc[2] = {v.s[mm].x, v.s[mm].y};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (((sc[e / 4] >> (8 * (e & 3))) & 255u) == 255u) {
+                    mine |= 1u << (16 * mm + 8 * eta + e);
+                    sc[e / 4] &= ~(255u << (8 * (e & 3)));
+                }
+            }
+            v.s[mm] = uintx2{sc[0], sc[1]};
+        }
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            const int src = b * (32 / NT);
+            bad[b] = (uint32_t)__shfl((int)mine, src, 64) | (uint32_t)__shfl((int)mine, src + 32, 64);
+        }
+        probabilities<JT, NT>(st, c, m, l, o, p);
+        add_values<DH, JT>(v, p, lr, o);
+        if (__any(mine != 0)) {
+            // A row i of a block holds dim NT i + t, of the 32-dim block NT i / 32; element e has i / 8 = e / 4
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+                for (int t2 = 0; t2 < NT; ++t2)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (seen[jt] & bad[(e / 4) * NT / 4]) o[jt][t2][e] = __uint_as_float(0x7FC00000u);
+        }
+        refill(i);
+    }
+    __builtin_amdgcn_s_waitcnt(0);   // no copy lands after this point
 
     // merge of the four waves
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) {
         l[jt] += __shfl_xor(l[jt], 32, 64);
         if (eta == 0) {
-            ml[wave][jt][0][lr] = m[jt];
-            ml[wave][jt][1][lr] = l[jt];
+            ml[(wave * JT + jt) * 64 + lr] = m[jt];
+            ml[(wave * JT + jt) * 64 + 32 + lr] = l[jt];
         }
     }
     floatx4* buf = reinterpret_cast<floatx4*>(smem);
@@ -298,11 +498,11 @@ __global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles
         __syncthreads();
         float mm = kFloor, f[4], ll = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, ml[w][jt][0][lr]);
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, ml[(w * JT + jt) * 64 + lr]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            f[w] = exp2_fast(ml[w][jt][0][lr] - mm);
-            ll += ml[w][jt][1][lr] * f[w];
+            f[w] = exp2_fast(ml[(w * JT + jt) * 64 + lr] - mm);
+            ll += ml[(w * JT + jt) * 64 + 32 + lr] * f[w];
         }
         // this wave: rows i = 8 wave + 4 eta + 0..3 of every block: dims NT (8 wave + 4 eta) + 0 .. 4 NT - 1
         float r[4][NT];
@@ -318,7 +518,7 @@ __global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles
         if (rho >= nrows) continue;
         const size_t row = ((size_t)s * R + rho % R) * a.Hq + kvh * GQ + rho / R;
         const int d0 = NT * (8 * wave + 4 * eta);
-        if (gridDim.y == 1) {
+        if (nsplit == 1) {
             const float inv = 1.f / ll;
             uint32_t w[2 * NT];
 #pragma unroll
@@ -328,7 +528,7 @@ __global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles
 #pragma unroll
             for (int i = 0; i < NT / 2; ++i) dst[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
         } else {
-            const size_t total = (size_t)a.b * R * a.Hq, at = (size_t)blockIdx.y * total + row;
+            const size_t total = (size_t)a.b * R * a.Hq, at = (size_t)split * total + row;
             float* dst = a.part + at * DH + d0;
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
@@ -338,7 +538,7 @@ __global__ __launch_bounds__(256) void attn_mx_kernel(MxAttnArgs a, int rowtiles
                 *reinterpret_cast<floatx4*>(dst + 4 * i) = x;
             }
             if (wave == 0 && eta == 0) {
-                float* pm = a.part + (size_t)gridDim.y * total * DH + at * 2;
+                float* pm = a.part + (size_t)nsplit * total * DH + at * 2;
                 pm[0] = mm;
                 pm[1] = ll;
             }
@@ -368,15 +568,14 @@ __global__ __launch_bounds__(256) void attn_mx_combine_kernel(const float* __res
 }
 
 struct Plan {
-    int rowtiles, split, tps;
+    int jt, rowtiles, split, tps;
 };
-
-constexpr int kRowsPerWave = 64;
 
 Plan plan_of(int b, int B, int Hq, int Hkv, int P) {
     Plan p;
     const int nrows = Hq / Hkv * 2 * B;
-    p.rowtiles = (nrows + kRowsPerWave - 1) / kRowsPerWave;
+    p.jt = nrows > 32 ? 2 : 1;
+    p.rowtiles = (nrows + 32 * p.jt - 1) / (32 * p.jt);
     const int ntiles = (P + 2 * B + kTileKeys - 1) / kTileKeys;
     const int64_t wgs = (int64_t)p.rowtiles * Hkv * b;
     p.split = 1;
@@ -391,6 +590,10 @@ Plan plan_of(int b, int B, int Hq, int Hkv, int P) {
     return p;
 }
 
+template <int DH, int JT> void run(const MxAttnArgs& a, const Plan& p, hipStream_t s) {
+    launch(attn_mx_kernel<DH, JT>, dim3((unsigned)(p.rowtiles * a.Hkv * a.b), p.split), dim3(256), 0, s, a, p.rowtiles, p.tps);
+}
+
 }  // namespace
 
 size_t attention_mx_partial_bytes(int b, int B, int Hq, int Hkv, int dh, int P) {
@@ -400,9 +603,13 @@ size_t attention_mx_partial_bytes(int b, int B, int Hq, int Hkv, int dh, int P) 
 
 hipError_t launch_attention_mx(const MxAttnArgs& a, hipStream_t s) {
     const Plan p = plan_of(a.b, a.B, a.Hq, a.Hkv, a.P);
-    const dim3 g((unsigned)(p.rowtiles * a.Hkv * a.b), p.split);
-    if (a.dh == 128) launch(attn_mx_kernel<128, kRowsPerWave / 32>, g, dim3(256), 0, s, a, p.rowtiles, p.tps);
-    else launch(attn_mx_kernel<64, kRowsPerWave / 32>, g, dim3(256), 0, s, a, p.rowtiles, p.tps);
+    if (a.dh == 128) {
+        if (p.jt == 2) run<128, 2>(a, p, s);
+        else run<128, 1>(a, p, s);
+    } else {
+        if (p.jt == 2) run<64, 2>(a, p, s);
+        else run<64, 1>(a, p, s);
+    }
     if (p.split > 1) {
         const int64_t rows = (int64_t)a.b * 2 * a.B * a.Hq;
         const dim3 gc((unsigned)((rows * (a.dh / 4) + 255) / 256));
