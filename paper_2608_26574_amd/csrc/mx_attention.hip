@@ -157,9 +157,9 @@ __device__ __forceinline__ int xcd_run(int id, int total) {
     return x * q + min(x, r) + (id >> 3);
 }
 
-// S^T = K Q^T of one tile.
+// S^T = K Q^T of one tile; q: the query operands in LDS, [JT][DH / 16][64 lanes].
 template <int DH, int JT>
-__device__ __forceinline__ void scores(const RawK<DH>& k, const bf16x8 (&q)[JT][DH / 16], floatx16 (&st)[JT]) {
+__device__ __forceinline__ void scores(const RawK<DH>& k, const bf16x8* q, int lane, floatx16 (&st)[JT]) {
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) st[jt] = floatx16{};
     const float f[2] = {scale_at<0>(k.s), scale_at<1>(k.s)};
@@ -169,7 +169,7 @@ __device__ __forceinline__ void scores(const RawK<DH>& k, const bf16x8 (&q)[JT][
         const bf16x8 kf = as_bf16x8(fp4x2_to_bf16x2<0>(x, f[j / 4]), fp4x2_to_bf16x2<1>(x, f[j / 4]),
                                     fp4x2_to_bf16x2<2>(x, f[j / 4]), fp4x2_to_bf16x2<3>(x, f[j / 4]));
 #pragma unroll
-        for (int jt = 0; jt < JT; ++jt) st[jt] = mfma32x32x16(kf, q[jt][j], st[jt]);
+        for (int jt = 0; jt < JT; ++jt) st[jt] = mfma32x32x16(kf, q[(jt * (DH / 16) + j) * 64 + lane], st[jt]);
     }
 }
 
@@ -257,18 +257,18 @@ __device__ __forceinline__ void add_values(const RawV& v, const uint32_t (&p)[JT
 }
 
 template <int DH, int JT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3 - JT)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
     constexpr int NJ = DH / 16, NT = DH / 32;
-    constexpr int kDepth = JT == 2 ? 7 : 4;            // tiles in flight per wave (one and two workgroups a CU)
+    constexpr int kDepth = DH == 128 ? 3 : 5;          // tiles in flight per wave (two workgroups share a CU)
     constexpr int kRing = kDepth * Slot<DH>::kBytes;
     static_assert(kDepth * Slot<DH>::kCopies <= 63, "vmcnt range");
-    static_assert(4 * kRing >= 4 * NT * 4 * 64 * 16, "the merge of the waves fits the rings");
+    constexpr int kMerge = NT * 4 * 64 * 16;           // O of one row tile of a wave
     // One array (several would carry alias information by which the compiler makes every LDS read
-    // wait for every copy in flight): the rings, which at the end hold O of one row tile of the four
-    // waves; the waves' maxima and sums; the rows' take-x words and their complements; the
+    // wait for every copy in flight): the rings and the query operands, in whose place O of one row
+    // tile of the four waves lies at the end; the waves' maxima and sums; the rows' take-x words and their complements; the
     // rows' visibility strings.
-    constexpr int kMl = 4 * kRing, kXs = kMl + 4 * JT * 64 * 4, kVis = kXs + 32 * JT * 2 * kBlockWords * 8;
+    constexpr int kQ = 4 * kRing, kMl = kQ + JT * NJ * 1024 > 4 * kMerge ? kQ + JT * NJ * 1024 : 4 * kMerge, kXs = kMl + 4 * JT * 64 * 4, kVis = kXs + 32 * JT * 2 * kBlockWords * 8;
     __shared__ __attribute__((aligned(16))) char smem[kVis + 32 * JT * kVisWords * 4];
     float* const ml = reinterpret_cast<float*>(smem + kMl);
     uint64_t* const xs = reinterpret_cast<uint64_t*>(smem + kXs);
@@ -289,14 +289,15 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
     const int nkeys = P + R, ntiles = (nkeys + kTileKeys - 1) / kTileKeys;
     const int t0 = split * tps, t1 = min(ntiles, t0 + tps);
 
-    // this lane's query rows: dims of the half eta
-    bf16x8 q[JT][NJ];
+    // query operands of the row tile, which the waves share: operand (jt, j), for lane l, holds row
+    // 32 jt + l % 32, the 8 dims from 8 j on of the half l / 32
+    bf16x8* const q = reinterpret_cast<bf16x8*>(smem + kQ);
+    bf16x8 qv[JT * NJ / 4];
 #pragma unroll
-    for (int jt = 0; jt < JT; ++jt) {
+    for (int i = 0; i < JT * NJ / 4; ++i) {
+        const int jt = (4 * i + wave) / NJ, j = (4 * i + wave) % NJ;
         const int rho = min(rt * 32 * JT + 32 * jt + lr, nrows - 1);
-        const bf16_t* qp = a.q + (((size_t)s * R + rho % R) * a.Hq + kvh * GQ + rho / R) * DH + eta * (DH / 2);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) q[jt][j] = ld_bf16x8(qp + 8 * j);
+        qv[i] = ld_bf16x8(a.q + (((size_t)s * R + rho % R) * a.Hq + kvh * GQ + rho / R) * DH + eta * (DH / 2) + 8 * j);
     }
     // states and confidences: of a row of the tile, and of a block position of word `wave`
     const bool block = t1 * kTileKeys > P && t0 < t1;   // (the same for the workgroup)
@@ -331,6 +332,8 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
         for (int i = 0; i < kDepth; ++i) tiles.copy(first + 4 * min(i, n - 1), ring + i * Slot<DH>::kBytes);
     }
     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < JT * NJ / 4; ++i) q[(4 * i + wave) * 64 + lane] = qv[i];
     // Visibility strings of the workgroup's rows, where its keys reach the block: wave w forms the
     // 64 positions from 64 w on of every row (a lane per row).  The rules are those of take_x:
     // ballots give the U and C sets, a candidate row compares its confidence with every candidate's.
@@ -366,9 +369,9 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
             const int start = 64 * (i % (kVisWords / 2));
             vis[i] = bits_at(w, start) | bits_at(w + kBlockWords, start - a.B);
         }
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
-        wg_barrier();
     }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
+    wg_barrier();
 
     const float c = a.scale * kLog2e;
     floatx16 o[JT][NT];
@@ -388,30 +391,17 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
         at = next_slot(at);
     };
     int i = 0;
-    if (full > 0) {
-        // while the probabilities of one tile are formed, the matrix cores run the scores of the next
-        floatx16 st[2][JT];
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm((kDepth - 1) * Slot<DH>::kCopies));
+    for (; i < full; ++i) {
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((kDepth - 1) * Slot<DH>::kCopies));   // tile i is there
         __builtin_amdgcn_sched_barrier(0);
-        scores<DH, JT>(read_k<DH>(ring, lane), q, st[0]);
-        auto step = [&](const floatx16 (&cur)[JT], floatx16 (&nxt)[JT]) __attribute__((always_inline)) {
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm((kDepth - 2) * Slot<DH>::kCopies));   // tiles i and i + 1 are there
-            __builtin_amdgcn_sched_barrier(0);
-            const RawK<DH> k = read_k<DH>(ring + next_slot(at) * Slot<DH>::kBytes, lane);
-            const RawV v = read_v<DH>(ring + at * Slot<DH>::kBytes, lane);
-            uint32_t p[JT][8];
-            scores<DH, JT>(k, q, nxt);
-            probabilities<JT, NT>(cur, c, m, l, o, p);
-            add_values<DH, JT>(v, p, lr, o);
-            refill(i);
-            ++i;
-        };
-        while (true) {
-            step(st[0], st[1]);
-            if (i == full) break;
-            step(st[1], st[0]);
-            if (i == full) break;
-        }
+        const RawK<DH> k = read_k<DH>(ring + at * Slot<DH>::kBytes, lane);
+        const RawV v = read_v<DH>(ring + at * Slot<DH>::kBytes, lane);
+        floatx16 st[JT];
+        uint32_t p[JT][8];
+        scores<DH, JT>(k, q, lane, st);
+        probabilities<JT, NT>(st, c, m, l, o, p);
+        add_values<DH, JT>(v, p, lr, o);
+        refill(i);
     }
     // tiles at the prefix's end and in the block
     for (; i < n; ++i) {
@@ -422,7 +412,7 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
         RawV v = read_v<DH>(ring + at * Slot<DH>::kBytes, lane);
         floatx16 st[JT];
         uint32_t p[JT][8], seen[JT];
-        scores<DH, JT>(k, q, st);
+        scores<DH, JT>(k, q, lane, st);
         // element 8 m + e of a lane is key k0 + 16 m + 8 eta + e
         const int j0 = k0 - P;
 #pragma unroll
@@ -567,6 +557,8 @@ __global__ __launch_bounds__(256) void attn_mx_combine_kernel(const float* __res
     reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
+constexpr int kSlots = 512;   // workgroups at once: two on each of 256 CUs
+
 struct Plan {
     int jt, rowtiles, split, tps;
 };
@@ -578,13 +570,10 @@ Plan plan_of(int b, int B, int Hq, int Hkv, int P) {
     p.rowtiles = (nrows + 32 * p.jt - 1) / (32 * p.jt);
     const int ntiles = (P + 2 * B + kTileKeys - 1) / kTileKeys;
     const int64_t wgs = (int64_t)p.rowtiles * Hkv * b;
-    p.split = 1;
-    if (wgs < 512) {
-        p.split = (int)((512 + wgs - 1) / wgs);
-        const int most = (ntiles + 7) / 8;   // two tiles a wave at least
-        p.split = p.split < most ? p.split : most;
-        p.split = p.split < 64 ? p.split : 64;
-    }
+    // one round of workgroups, two tiles a wave at least
+    const int64_t room = kSlots / wgs;
+    const int most = (ntiles + 7) / 8;
+    p.split = (int)(room < most ? (room > 1 ? room : 1) : most);
     p.tps = (ntiles + p.split - 1) / p.split;
     p.split = (ntiles + p.tps - 1) / p.tps;
     return p;
