@@ -264,73 +264,97 @@ def dard_linear(X, Wp, N, Y, stream=None):
 
 def _mx_check(rows, K, format, codes, scales):
     """codes and scales of `rows` rows of K values."""
-    if format not in (MX_FP8, MX_FP4):
+    if format != MX_FP8 and format != MX_FP4:
         raise ValueError(f"unknown MX format {format!r}")
     if K % MX_BLOCK:
         raise ValueError(f"MX rows hold whole blocks of {MX_BLOCK} values, got {K}")
-    want = rows * (K if format == MX_FP8 else K // 2)
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
         raise ValueError("MX codes and scales are uint8 tensors")
+    want = rows * (K if format == MX_FP8 else K // 2)
     if codes.numel() != want or scales.numel() != rows * (K // MX_BLOCK):
         raise ValueError(f"need {want} code bytes and {rows * (K // MX_BLOCK)} scales for {rows} rows of {K}, got "
                          f"{codes.numel()} and {scales.numel()}")
 
 
 def _mx_dt(t, what):
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{what} must be bfloat16 or float32, got {t.dtype}")
-    return _dt(t)
+    if t.dtype is torch.bfloat16:
+        return DTYPE_BF16
+    if t.dtype is torch.float32:
+        return DTYPE_F32
+    raise ValueError(f"{what} must be bfloat16 or float32, got {t.dtype}")
 
 
-def _here(*tensors):
-    """The tensors must be on the device whose stream the call uses."""
-    cur = torch.cuda.current_device() if torch.cuda.is_available() else None
+def _args(stream, tensors, strided=()):
+    """Device pointers of contiguous tensors (None -> NULL), then of `strided` ones, and the HIP stream
+    of the call.  All must be on the current device: kernels launch there."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -1
+    ptrs = []
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != cur:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{cur}")
+        if t is None:
+            ptrs.append(None)
+            continue
+        if not t.is_contiguous():
+            raise ValueError("libdard takes contiguous tensors")
+        ptrs.append(t)
+    ptrs += strided
+    for i, t in enumerate(ptrs):
+        if t is None:
+            continue
+        d = t.get_device()
+        if d < 0:
+            raise ValueError("libdard takes device tensors")
+        if d != dev:
+            raise ValueError(f"tensor on cuda:{d}, but the current device is cuda:{dev}")
+        ptrs[i] = t.data_ptr()
+    if stream is None:
+        return ptrs, torch._C._cuda_getCurrentRawStream(dev)
+    return ptrs, _stream(stream)
 
 
-def _rows_p(t, what):
-    """(pointer, leading dimension) of a [rows][K] tensor whose rows are contiguous."""
-    if not t.is_cuda:
-        raise ValueError("libdard takes device tensors")
+def _rows_ld(t, what):
+    """Leading dimension of a [rows][K] tensor whose rows are contiguous."""
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what} must be [rows][K] with contiguous rows")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _nbytes(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
 
 
 def dard_quantize_mx(x, format, codes, scales, stream=None):
     """x [rows][K] (bf16 or float32, rows may be further apart) to MX codes
     (uint8 [rows][K] or, MX_FP4, [rows][K/2]) and scales (uint8 [rows][K/32])."""
-    _here(x, codes, scales)
-    p, ld = _rows_p(x, "x")
-    _mx_check(x.shape[0], x.shape[1], format, codes, scales)
-    _check(lib().dard_quantize_mx(_mx_dt(x, "x"), p, ld, x.shape[0], x.shape[1], format, _p(codes), _p(scales),
-                                  _stream(stream)))
+    ld = _rows_ld(x, "x")
+    rows, K = x.shape
+    _mx_check(rows, K, format, codes, scales)
+    dt = _mx_dt(x, "x")
+    (c, s, p), st = _args(stream, (codes, scales), (x,))
+    _check(lib().dard_quantize_mx(dt, p, ld, rows, K, format, c, s, st))
 
 
 def dard_dequantize_mx(format, codes, scales, x, stream=None):
     """The values of MX codes and scales into x [rows][K] (bf16 or float32)."""
-    _here(x, codes, scales)
-    p, ld = _rows_p(x, "x")
-    _mx_check(x.shape[0], x.shape[1], format, codes, scales)
-    _check(lib().dard_dequantize_mx(format, _p(codes), _p(scales), x.shape[0], x.shape[1], _mx_dt(x, "x"), p, ld,
-                                    _stream(stream)))
+    ld = _rows_ld(x, "x")
+    rows, K = x.shape
+    _mx_check(rows, K, format, codes, scales)
+    dt = _mx_dt(x, "x")
+    (c, s, p), st = _args(stream, (codes, scales), (x,))
+    _check(lib().dard_dequantize_mx(format, c, s, rows, K, dt, p, ld, st))
 
 
 def dard_resid_norm_mx(h, gain, eps, format, codes, scales, delta=None, stream=None):
     """h [rows][d] float32 += delta (bf16 or float32, or None); the RMS norm of
     its rows times gain in MX."""
-    _here(h, gain, codes, scales, delta)
     rows, d = h.shape
-    if h.dtype != torch.float32:
+    if h.dtype is not torch.float32:
         raise ValueError("h must be float32")
-    if gain.numel() != d or (delta is not None and tuple(delta.shape) != (rows, d)):
+    if gain.numel() != d or (delta is not None and delta.shape != h.shape):
         raise ValueError(f"need gain [{d}] and delta [{rows}][{d}]")
     _mx_check(rows, d, format, codes, scales)
-    _check(lib().dard_resid_norm_mx(_p(h), DTYPE_F32 if delta is None else _mx_dt(delta, "delta"), _p(delta),
-                                    _mx_dt(gain, "gain"), _p(gain), eps, rows, d, format, _p(codes), _p(scales),
-                                    _stream(stream)))
+    ddt, gdt = DTYPE_F32 if delta is None else _mx_dt(delta, "delta"), _mx_dt(gain, "gain")
+    (hp, dp, gp, c, s), st = _args(stream, (h, delta, gain, codes, scales))
+    _check(lib().dard_resid_norm_mx(hp, ddt, dp, gdt, gp, eps, rows, d, format, c, s, st))
 
 
 def dard_packed_mx_bytes(N, K):
@@ -343,12 +367,12 @@ def dard_packed_mx_bytes(N, K):
 def dard_pack_matrix_mx(codes, scales, Wp, stream=None):
     """Lay out MXFP4 weights (codes [N][K/2], scales [N][K/32]) for dard_linear_mx;
     Wp: uint8 [dard_packed_mx_bytes(N, K)]."""
-    _here(codes, scales, Wp)
     N, K = codes.shape[0], 2 * codes.shape[1]
     _mx_check(N, K, MX_FP4, codes, scales)
-    if Wp.numel() * Wp.element_size() < dard_packed_mx_bytes(N, K):
+    if _nbytes(Wp) < dard_packed_mx_bytes(N, K):
         raise ValueError(f"Wp needs {dard_packed_mx_bytes(N, K)} bytes")
-    _check(lib().dard_pack_matrix_mx(_p(codes), _p(scales), N, K, _p(Wp), _stream(stream)))
+    (c, s, w), st = _args(stream, (codes, scales, Wp))
+    _check(lib().dard_pack_matrix_mx(c, s, N, K, w, st))
 
 
 def dard_linear_mx_workspace_bytes(format, M, N, K):
@@ -358,73 +382,70 @@ def dard_linear_mx_workspace_bytes(format, M, N, K):
 def dard_linear_mx(format, codes, scales, Wp, Y, ws=None, stream=None):
     """Y [M][N] (bf16 or float32) = X W^T, X in MX (codes [M][K] or [M][K/2],
     scales [M][K/32]), W packed by dard_pack_matrix_mx."""
-    _here(codes, scales, Wp, Y, ws)
     M, N = Y.shape
     K = codes.shape[1] * (1 if format == MX_FP8 else 2)
     _mx_check(M, K, format, codes, scales)
-    if Wp.numel() * Wp.element_size() < dard_packed_mx_bytes(N, K):
-        raise ValueError(f"Wp of {Wp.numel()} bytes does not hold a packed [{N}][{K}] matrix")
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
-    _check(lib().dard_linear_mx(format, _p(codes), _p(scales), M, K, _p(Wp), N, _mx_dt(Y, "Y"), _p(Y), _p(ws), nbytes,
-                                _stream(stream)))
+    if _nbytes(Wp) < dard_packed_mx_bytes(N, K):
+        raise ValueError(f"Wp of {_nbytes(Wp)} bytes does not hold a packed [{N}][{K}] matrix")
+    dt = _mx_dt(Y, "Y")
+    (c, s, w, y, room), st = _args(stream, (codes, scales, Wp, Y, ws))
+    _check(lib().dard_linear_mx(format, c, s, M, K, w, N, dt, y, room, _nbytes(ws), st))
 
 
 def _mx_cache(cache, b, Hkv, dh):
-    """(cap, pointers) of an MXFP4 cache (kc, ks, vc, vs) of b sequences."""
+    """Capacity of an MXFP4 cache (kc, ks, vc, vs) of b sequences."""
     kc, ks, vc, vs = cache
-    _here(*cache)
     if kc.dim() != 4:
         raise ValueError("kc must be [b][Hkv][cap][dh/2]")
     cap = kc.shape[2]
     want = ((b, Hkv, cap, dh // 2), (b, Hkv, cap, dh // 32), (b, Hkv, cap // 8, dh // 4, 8, 2),
             (b, Hkv, cap // 8, dh // 32, 8))
     for name, t, shape in zip(("kc", "ks", "vc", "vs"), cache, want):
-        if tuple(t.shape) != shape or t.dtype != torch.uint8:
+        if t.shape != shape or t.dtype is not torch.uint8:
             raise ValueError(f"{name} must be uint8 {shape}, got {t.dtype} {tuple(t.shape)}")
-    return cap, [_p(t) for t in cache]
+    return cap
 
 
 def _mx_prefix(prefix, b):
-    if prefix is not None and (prefix.dtype != torch.int32 or prefix.numel() != b):
+    if prefix is not None and (prefix.dtype is not torch.int32 or prefix.numel() != b):
         raise ValueError(f"prefix must be int32 [{b}]")
-    _here(prefix)
-    return _p(prefix)
+    return prefix
 
 
-def _tokens_p(t, what):
-    """(pointer, elements between tokens) of a [b][n][Hkv][dh] tensor whose heads are contiguous."""
+def _tokens_ld(t, what):
+    """Elements between the tokens of a [b][n][Hkv][dh] tensor whose heads are contiguous."""
     b, n, Hkv, dh = t.shape
-    if not t.is_cuda:
-        raise ValueError("libdard takes device tensors")
-    ld = t.stride(1) if n > 1 else (t.stride(0) if b > 1 else Hkv * dh)
-    if (dh > 1 and t.stride(3) != 1) or (Hkv > 1 and t.stride(2) != dh) or (b > 1 and t.stride(0) != n * ld):
+    sb, sn, sh, sd = t.stride()
+    ld = sn if n > 1 else (sb if b > 1 else Hkv * dh)
+    if (dh > 1 and sd != 1) or (Hkv > 1 and sh != dh) or (b > 1 and sb != n * ld):
         raise ValueError(f"{what} must be [b][n][Hkv][dh] with contiguous heads and evenly spaced tokens")
-    return t.data_ptr(), ld
+    return ld
 
 
-def _kv_args(cache, pos, k, v, prefix):
-    if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 4:
+def _kv_args(cache, k, v, prefix, stream):
+    if k.shape != v.shape or k.dtype is not v.dtype or k.dim() != 4:
         raise ValueError("k and v must be [b][n][Hkv][dh] tensors of one type")
     b, n, Hkv, dh = k.shape
-    _here(k, v)
-    cap, ptrs = _mx_cache(cache, b, Hkv, dh)
-    (kp, ld), (vp, ldv) = _tokens_p(k, "k"), _tokens_p(v, "v")
-    if ld != ldv:
+    cap = _mx_cache(cache, b, Hkv, dh)
+    ld = _tokens_ld(k, "k")
+    if _tokens_ld(v, "v") != ld:
         raise ValueError("k and v must have the same distance between tokens")
-    return b, n, Hkv, dh, cap, ptrs, kp, vp, ld, _mx_dt(k, "k"), _mx_prefix(prefix, b)
+    dt = _mx_dt(k, "k")
+    ptrs, st = _args(stream, (*cache, _mx_prefix(prefix, b)), (k, v))
+    return b, n, Hkv, dh, cap, ld, dt, ptrs, st
 
 
 def dard_kv_write_mx(k, v, cache, pos, prefix=None, stream=None):
     """k, v [b][n][Hkv][dh] (bf16 or float32; slices of a wider row will do) into
     the MXFP4 cache (kc, ks, vc, vs) at keys pos.. (or prefix[s]..)."""
-    b, n, Hkv, dh, cap, ptrs, kp, vp, ld, dt, pre = _kv_args(cache, pos, k, v, prefix)
-    _check(lib().dard_kv_write_mx(dt, kp, vp, ld, b, n, Hkv, dh, pos, pre, cap, *ptrs, _stream(stream)))
+    b, n, Hkv, dh, cap, ld, dt, (kc, ks, vc, vs, pre, kp, vp), st = _kv_args(cache, k, v, prefix, stream)
+    _check(lib().dard_kv_write_mx(dt, kp, vp, ld, b, n, Hkv, dh, pos, pre, cap, kc, ks, vc, vs, st))
 
 
 def dard_kv_read_mx(cache, pos, k, v, prefix=None, stream=None):
     """The values of keys pos.. (or prefix[s]..) of the cache into k, v [b][n][Hkv][dh]."""
-    b, n, Hkv, dh, cap, ptrs, kp, vp, ld, dt, pre = _kv_args(cache, pos, k, v, prefix)
-    _check(lib().dard_kv_read_mx(*ptrs, cap, b, n, Hkv, dh, pos, pre, dt, kp, vp, ld, _stream(stream)))
+    b, n, Hkv, dh, cap, ld, dt, (kc, ks, vc, vs, pre, kp, vp), st = _kv_args(cache, k, v, prefix, stream)
+    _check(lib().dard_kv_read_mx(kc, ks, vc, vs, cap, b, n, Hkv, dh, pos, pre, dt, kp, vp, ld, st))
 
 
 def dard_attention_mx_workspace_bytes(b, B, Hq, Hkv, dh, P):
@@ -434,19 +455,18 @@ def dard_attention_mx_workspace_bytes(b, B, Hq, Hkv, dh, P):
 def dard_masked_attention_mx(q, cache, P, state, conf, scale, flags, out, ws=None, prefix=None, stream=None):
     """dard_masked_attention over an MXFP4 cache (kc, ks, vc, vs); prefix: int32
     [b] prefix lengths of the sequences (at most P), or None: P each."""
-    _here(q, state, conf, out, ws)
     b, R, Hq, dh = q.shape
-    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape != q.shape:
+    if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or out.shape != q.shape:
         raise ValueError("q and out must be bfloat16 [b][2B][Hq][dh]")
-    if R % 2 or tuple(state.shape) != (b, R // 2) or tuple(conf.shape) != (b, R // 2):
+    if R % 2 or state.shape != (b, R // 2) or conf.shape != state.shape:
         raise ValueError(f"state and conf must be [b][B] = {(b, R // 2)}")
-    if state.dtype != torch.uint8 or conf.dtype != torch.float32:
+    if state.dtype is not torch.uint8 or conf.dtype is not torch.float32:
         raise ValueError("state must be uint8, conf float32")
     Hkv = cache[0].shape[1]
-    cap, ptrs = _mx_cache(cache, b, Hkv, dh)
-    nbytes = ws.numel() * ws.element_size() if ws is not None else 0
-    _check(lib().dard_masked_attention_mx(_p(q), *ptrs, P, _mx_prefix(prefix, b), cap, _p(state), _p(conf), b, R // 2, Hq,
-                                          Hkv, dh, scale, flags, _p(out), _p(ws), nbytes, _stream(stream)))
+    cap = _mx_cache(cache, b, Hkv, dh)
+    (qp, kc, ks, vc, vs, pre, sp, cp, op, room), st = _args(stream, (q, *cache, _mx_prefix(prefix, b), state, conf, out, ws))
+    _check(lib().dard_masked_attention_mx(qp, kc, ks, vc, vs, P, pre, cap, sp, cp, b, R // 2, Hq, Hkv, dh, scale, flags,
+                                          op, room, _nbytes(ws), st))
 
 
 def dard_trace_enable(mask):
