@@ -10,6 +10,8 @@
 // aligned to the largest and cut 13 bits below its leading one (measured: a
 // power of two 2^-14 of it no longer counts, neither does anything past 23 bits
 // below the sum it is added to).
+#include <type_traits>
+
 #include "launch.h"
 #include "mx.h"
 
@@ -152,6 +154,195 @@ __global__ __launch_bounds__(64 * NW) void linear_mx_kernel(LinArgs a) {
     }
 }
 
+// ---------------------------------------------------------------- tiles
+// From 65 rows on.  A workgroup of 2 x 2 waves owns a 64 TI x 64 TJ tile, a wave 32 TI x 32 TJ
+// of it; both operands go through LDS in stages of 128 k, NST deep, copied
+// straight from memory.  Packed weights are in operand order already; rows of x
+// are swizzled in 16-byte chunks by which lane of a copy fetches which chunk: row r
+// keeps chunk c in slot c ^ f(r), f(r) = r / 2 (E4M3, 128 bytes a row) or r / 4 (E2M1,
+// 64 bytes), so the 16 lanes that LDS serves at once hit 16 different
+// 16-byte columns of its 256.  Scales go to registers, a unit ahead.
+// The fragments of each 64-k step are read during the step before; the barrier of
+// a stage stands between its two steps, where every wave holds the rest of the stage
+// in registers, publishes the next stage and frees this one for a copy.
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));   // (typed: see mx_attention.hip)
+
+__device__ __forceinline__ void copy16_lds(__amdgpu_buffer_rsrc_t r, char* dst, int voff) {
+#if __HIP_DEVICE_COMPILE__   // (the host pass does not know the builtin)
+    typedef __attribute__((address_space(3))) void* lds_ptr;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)dst, 16, voff, 0, 0, 0);
+#endif
+}
+
+template <int F, int TI, int TJ, int NST, int OCC>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+void linear_mx_tile_kernel(LinArgs a, int tiles_m, int tiles_n) {
+    constexpr bool F8 = F == DARD_MX_FP8;
+    constexpr int BM = 64 * TI, BN = 64 * TJ;
+    constexpr int RB = F8 ? 128 : 64, CPR = RB / 16;         // bytes and chunks of a row of x per stage
+    constexpr int XB = BM * RB, WB = BN * 64, STAGE = XB + WB;
+    constexpr int CX = XB / 4096, CW = WB / 4096, CP = CX + CW;   // copies of a wave per stage
+    static_assert((NST - 1) * CP <= 63, "vmcnt range");
+    __shared__ __attribute__((aligned(16))) char smem[NST * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1, lr = lane & 31, eta = lane >> 5;
+    // Tile order: each XCD a contiguous run of an order that walks groups of eight row tiles column
+    // by column, so that the tiles in flight on an XCD share rows and weights in its L2.
+    const int total = tiles_m * tiles_n;
+    const int id = blockIdx.x, xcd = id & 7;
+    const int t = xcd * (total >> 3) + min(xcd, total & 7) + (id >> 3);
+    constexpr int GM = 8;
+    const int grp = t / (GM * tiles_n), in = t - grp * GM * tiles_n, gm = min(GM, tiles_m - grp * GM);
+    const int m0 = (grp * GM + in % gm) * BM, n0 = in / gm * BN;
+    const int units = a.KBp / 8;
+    const int u0 = (int)((int64_t)units * blockIdx.y / gridDim.y), u1 = (int)((int64_t)units * (blockIdx.y + 1) / gridDim.y);
+    const int ns = 2 * (u1 - u0);                            // stages
+    const int KB = a.K / 32, rowb = F8 ? a.K : a.K / 2;      // scales and code bytes of a row of x
+
+    // Copies: chunk q of a stage's image is lane q % 64 of copy q / 64.  Reads past the
+    // descriptor's end give zeros: rows past M, and k past K by an offset outside.
+    const int64_t left = (int64_t)(a.M - m0) * rowb;
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(a.xc + (size_t)m0 * rowb), (short)0, (int)(left < 0xFFFFFF00ll ? left : 0xFFFFFF00ll), 0x00020000);
+    const int blk0 = n0 / 32;
+    // Copy j of a wave fetches rows (wave CX + j) RPC + lane / CPR; f(row), and with it the lane's chunk,
+    // depends on j's parity at most.
+    constexpr int RPC = 64 / CPR;
+    static_assert(CX % 2 == 0, "parities of j");
+    int xk[2], xo[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int row = (wave * CX + j) * RPC + lane / CPR;
+        xk[j] = 16 * ((lane % CPR) ^ ((F8 ? row >> 1 : row >> 2) & (CPR - 1)));
+        xo[j] = (wave * CX * RPC + lane / CPR) * rowb + xk[j];
+    }
+    auto copy = [&](int st, int slot) __attribute__((always_inline)) {   // stage st (128 k each; past the last: repeated)
+        const int s2 = 2 * u0 + min(st, ns - 1), kb = s2 * RB;
+        char* dst = smem + slot * STAGE;
+#pragma unroll
+        for (int j = 0; j < CX; ++j) {
+            const int o = kb + xk[j & 1] < rowb ? xo[j & 1] + (kb + j * RPC * rowb) : -16;
+            copy16_lds(rx, dst + (wave * CX + j) * 1024, o);
+        }
+#pragma unroll
+        for (int j = 0; j < CW; ++j) {
+            // 1 KB of the packed codes: two k blocks of 32 rows (block b of the tile, half h of the stage)
+            const int q = wave * CW + j, b = q >> 1, h = q & 1;
+            const size_t blk = min(blk0 + b, a.nblk - 1);
+            const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
+                (void*)(a.wc + (blk * a.KBp + 4 * s2 + 2 * h) * 512), (short)0, 1024, 0x00020000);
+            copy16_lds(rw, dst + XB + q * 1024, 16 * lane);
+        }
+    };
+    // scales of a unit (two stages)
+    const uint8_t* const xs0 = a.xs + (size_t)m0 * KB;
+    int xso[TI];
+#pragma unroll
+    for (int i = 0; i < TI; ++i) xso[i] = min(32 * (wm * TI + i) + lr, a.M - 1 - m0) * KB;
+    uint32_t sx[2][TI], sw[2][TJ];
+    auto load_scales = [&](int u, uint32_t (&x)[TI], uint32_t (&w)[TJ]) __attribute__((always_inline)) {
+        const int uu = min(u, u1 - 1);
+#pragma unroll
+        for (int i = 0; i < TI; ++i) x[i] = ld_xs(xs0 + xso[i], uu, eta, KB);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+            const size_t blk = min(blk0 + wn * TJ + j, a.nblk - 1);
+            w[j] = a.ws[(blk * (a.KBp / 8) + uu) * 64 + lane];
+        }
+    };
+
+    floatx16 acc[TI][TJ];
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) acc[i][j] = floatx16{};
+    struct Frag {
+        uintx4 x[TI][F8 ? 2 : 1], w[TJ];
+    };
+    auto read = [&](Frag& f, int slot, int h) __attribute__((always_inline)) {
+        const char* st = smem + slot * STAGE;
+#pragma unroll
+        for (int i = 0; i < TI; ++i) {
+            const int row = 32 * (wm * TI + i) + lr, sz = (F8 ? row >> 1 : row >> 2) & (CPR - 1);
+            if constexpr (F8) {
+                f.x[i][0] = *reinterpret_cast<const uintx4*>(st + row * RB + 16 * ((4 * h + eta) ^ sz));
+                f.x[i][1] = *reinterpret_cast<const uintx4*>(st + row * RB + 16 * ((4 * h + 2 + eta) ^ sz));
+            } else {
+                f.x[i][0] = *reinterpret_cast<const uintx4*>(st + row * RB + 16 * ((2 * h + eta) ^ sz));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+            f.w[j] = *reinterpret_cast<const uintx4*>(st + XB + ((wn * TJ + j) * 2 + h) * 1024 + 16 * lane);
+    };
+    auto mm = [&](const Frag& f, const uint32_t (&x)[TI], const uint32_t (&w)[TJ], auto jc) __attribute__((always_inline)) {
+        constexpr int J = decltype(jc)::value;
+        intx8 wv[TJ];
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) wv[j] = intx8{(int)f.w[j][0], (int)f.w[j][1], (int)f.w[j][2], (int)f.w[j][3], 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < TI; ++i) {
+            const uintx4 lo = f.x[i][0], hi = F8 ? f.x[i][F8 ? 1 : 0] : uintx4{0, 0, 0, 0};
+            const intx8 xv = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] = mfma_mx<F, J>(xv, wv[j], acc[i][j], x[i], w[j]);
+        }
+    };
+
+    load_scales(u0, sx[0], sw[0]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int p = 0; p < NST; ++p) copy(p, p);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 1) * CP));
+    wg_barrier();
+    Frag f0, f1;
+    read(f0, 0, 0);
+    int slot = 0;
+    // a stage: steps J and J + 1 of its unit
+    auto stage = [&](int st, const uint32_t (&x)[TI], const uint32_t (&w)[TJ], auto jc) __attribute__((always_inline)) {
+        constexpr int J = decltype(jc)::value;
+        const int next = slot + 1 == NST ? 0 : slot + 1;
+        read(f1, slot, 1);
+        mm(f0, x, w, std::integral_constant<int, J>{});
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm((NST - 2) * CP));   // stage st + 1 is there; every read of this one is done
+        wg_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        copy(st + NST, slot);
+        read(f0, next, 0);
+        mm(f1, x, w, std::integral_constant<int, J + 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+        slot = next;
+    };
+    for (int u = u0, st = 0; u < u1; ++u, st += 2) {
+        load_scales(u + 1, sx[1], sw[1]);
+        stage(st, sx[0], sw[0], std::integral_constant<int, 0>{});
+        stage(st + 1, sx[0], sw[0], std::integral_constant<int, 2>{});
+#pragma unroll
+        for (int i = 0; i < TI; ++i) sx[0][i] = sx[1][i];
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) sw[0][j] = sw[1][j];
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));   // no copy lands after this point
+
+    // element v of a lane: row 8 (v / 4) + 4 eta + v % 4, column lane % 32
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+            const int n = n0 + 32 * (wn * TJ + j) + lr, mb = m0 + 32 * (wm * TI + i) + 4 * eta;
+            if (n >= a.N) continue;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int m = mb + 8 * (v / 4) + v % 4;
+                if (m >= a.M) continue;
+                if (gridDim.y > 1) a.part[((size_t)blockIdx.y * a.M + m) * a.N + n] = acc[i][j][v];
+                else st_y(a, m, n, acc[i][j][v]);
+            }
+        }
+}
+
 // Sum of the K splits' partials, in split order.
 __global__ __launch_bounds__(256) void linear_mx_sum_kernel(LinArgs a, int nsplit, int64_t total) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -162,22 +353,42 @@ __global__ __launch_bounds__(256) void linear_mx_sum_kernel(LinArgs a, int nspli
     else reinterpret_cast<float*>(a.y)[i] = v;
 }
 
+// Kernel, tile and K split of a product.
 struct Plan {
+    int ti, tj;          // tile of 64 ti x 64 tj (tiled kernel), or ti = 0: the streaming kernel
     int nt, mt, split;
 };
 
 Plan plan_of(int, int M, int N, int K) {
-    Plan p;
-    p.nt = (N + 63) / 64;
-    p.mt = (M + 63) / 64;
+    Plan p{};
     const int units = (K / 32 + 7) / 8;
     p.split = 1;
-    while (p.nt * p.mt * p.split < 256 && units / (p.split * 2 * 4) >= 1 && p.split < 8) p.split *= 2;
+    if (M <= 64) {
+        p.nt = (N + 63) / 64;
+        p.mt = (M + 63) / 64;
+        while (p.nt * p.mt * p.split < 256 && units / (p.split * 2 * 4) >= 1 && p.split < 8) p.split *= 2;
+        return p;
+    }
+    p.ti = p.tj = 4;
+    p.mt = (M + 255) / 256;
+    p.nt = (N + 255) / 256;
+    if (p.mt * p.nt < 192) {
+        p.ti = p.tj = 2;
+        p.mt = (M + 127) / 128;
+        p.nt = (N + 127) / 128;
+        while (p.nt * p.mt * p.split < 256 && units / (p.split * 2) >= 4 && p.split < 8) p.split *= 2;
+    }
     return p;
 }
 
 template <int F> void run(const LinArgs& a, const Plan& p, hipStream_t s) {
-    launch(linear_mx_kernel<F, 2, 2, 4>, dim3(p.nt, p.mt, p.split), dim3(256), 0, s, a);
+    constexpr int kDeep = F == DARD_MX_FP8 ? 3 : 4;
+    if (p.ti == 4)
+        launch(linear_mx_tile_kernel<F, 4, 4, kDeep, 1>, dim3(p.nt * p.mt, p.split), dim3(256), 0, s, a, p.mt, p.nt);
+    else if (p.ti == 2)
+        launch(linear_mx_tile_kernel<F, 2, 2, kDeep, 2>, dim3(p.nt * p.mt, p.split), dim3(256), 0, s, a, p.mt, p.nt);
+    else
+        launch(linear_mx_kernel<F, 2, 2, 4>, dim3(p.nt, p.mt, p.split), dim3(256), 0, s, a);
 }
 
 }  // namespace
