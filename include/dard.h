@@ -482,7 +482,8 @@ dard_status dard_gemm_plan(int dtype, int M, int N, int K, int partial, int frag
  * -127, which is also the exponent of a block of zeros; the elements are
  * x / scale rounded to nearest, ties to the even code, saturating at 448 or 6.
  * A block that holds an infinity or a NaN gets the scale 255 and zero codes.
- * Code arrays are 16-byte aligned (other arrays, and x, as their element).
+ * Code arrays are 16-byte aligned (other arrays, and x, as their element).  A
+ * call takes rows * K < 2^34 values.
  *
  *   dard_quantize_mx    x [rows][K] float32 or bf16, rows ld elements apart
  *                       (ld >= K); codes and scales contiguous.
@@ -505,22 +506,28 @@ dard_status dard_dequantize_mx(int format, const void* codes, const uint8_t* sca
  * does not depend on how the kernel splits a row.
  * h [rows][d] float32, updated in place; delta [rows][d] float32 or bf16
  * (delta_dtype) or NULL; gain [d] float32 or bf16 (gain_dtype).  Needs
- * d % 32 == 0, d <= 8192.  A row with an infinity or a NaN gives NaN blocks. */
+ * d % 32 == 0, d <= 8192, rows < 2^24.  A row with an infinity or a NaN gives NaN blocks. */
 dard_status dard_resid_norm_mx(float* h, int delta_dtype, const void* delta, int gain_dtype,
                                const void* gain, float eps, int rows, int d, int format, void* codes,
                                uint8_t* scales, void* stream);
 
 /* Product with MXFP4 weights:  Y[m][n] = sum_k x[m][k] w[n][k], both in MX,
- * accumulated in float32 by the scaled matrix instructions and rounded once
- * when Y is bf16.  Those align the products of eight consecutive k to the
- * largest of them before they add and keep 13 bits below its leading one.
+ * summed in float32.
+ *   Y float32 of an MXFP8 x: products exact, sums float32's (values of x below
+ *   2^-126 count to multiples of 2^-133; results of a row of x or w with scale
+ *   codes from 240 on, which float32 values never quantise to, are as below);
+ *   Y bf16 (one more rounding), or an MXFP4 x: the products of eight consecutive
+ *   k are aligned to the largest of them before they are added and keep 13 bits
+ *   below its leading one (of MXFP4 products of one scale no bit is lost).
  * dard_pack_matrix_mx() lays a quantised W (DARD_MX_FP4 codes [N][K/2], scales
  * [N][K/32]) out in the order the kernels read it (not a hot call); Wp holds
  * dard_packed_mx_bytes(N, K) bytes, 16-byte aligned.
  * dard_linear_mx: x [M][K] in `format`; Y [M][N] float32 or bf16 (out_dtype).
- * Needs M, N >= 1, K % 32 == 0 and a W under 2^31 codes bytes; any N.
+ * Needs M, N >= 1, K % 32 == 0, K <= 2^20, M * N < 2^39 and a W under 2^31 code
+ * bytes; any N.
  * Workspace: dard_linear_mx_workspace_bytes(...) bytes, 16-byte aligned (0: none
- * is needed, ws may be NULL); its contents need no initialisation. */
+ * is needed, ws may be NULL, which holds for every product of this version); its
+ * contents need no initialisation. */
 size_t dard_packed_mx_bytes(int N, int K);
 dard_status dard_pack_matrix_mx(const void* codes, const uint8_t* scales, int N, int K, void* Wp,
                                 void* stream);

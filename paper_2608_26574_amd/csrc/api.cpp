@@ -486,7 +486,7 @@ dard_status dard_resid_norm_mx(float* h, int delta_dtype, const void* delta, int
     if (!gain) return fail(DARD_ERR_ARG, "NULL pointer");
     if (!(eps >= 0.f)) return fail(DARD_ERR_ARG, "need eps >= 0");
     if (int rc = check_mx_rows(h, DARD_DTYPE_F32, d, rows, d, codes, scales)) return rc;
-    if (d > 8192) return fail(DARD_ERR_SHAPE, "d must be <= 8192");
+    if (d > 8192 || rows >= 1 << 24) return fail(DARD_ERR_SHAPE, "need d <= 8192 and rows < 2^24");
     if (!aligned(gain, esize(gain_dtype)) || (delta && !aligned(delta, esize(delta_dtype))))
         return fail(DARD_ERR_ARG, "gain and delta must be aligned to their element");
     TraceScope ts(DARD_K_NORM, (hipStream_t)stream);
@@ -500,7 +500,15 @@ namespace {
 int check_mx_weight(int N, int K) {
     if (N < 1 || K < 32 || K % 32) return fail(DARD_ERR_SHAPE, "need N >= 1 and K %% 32 == 0");
     const MxPacked p = mx_packed(N, K);
+    if (K > 1 << 20) return fail(DARD_ERR_SHAPE, "need K <= 2^20");
     if (p.scales > 0x7FFFFFFFull) return fail(DARD_ERR_SHAPE, "the packed codes of a weight must be under 2 GiB");
+    return DARD_OK;
+}
+
+int check_mx_product(int M, int N, int K) {
+    if (M < 1) return fail(DARD_ERR_SHAPE, "need M >= 1");
+    if (int rc = check_mx_weight(N, K)) return rc;
+    if ((int64_t)M * N >= (int64_t)1 << 39) return fail(DARD_ERR_SHAPE, "need M * N < 2^39");
     return DARD_OK;
 }
 
@@ -517,23 +525,18 @@ dard_status dard_pack_matrix_mx(const void* codes, const uint8_t* scales, int N,
 }
 
 size_t dard_linear_mx_workspace_bytes(int format, int M, int N, int K) {
-    if (check_mx_types(format, DARD_DTYPE_F32) || M < 1 || check_mx_weight(N, K)) return 0;
-    return linear_mx_partial_bytes(format, M, N, K);
+    if (!check_mx_types(format, DARD_DTYPE_F32)) check_mx_product(M, N, K);   // (for the error it records)
+    return 0;   // (every kernel merges its parts of K in LDS)
 }
 
 dard_status dard_linear_mx(int format, const void* codes, const uint8_t* scales, int M, int K, const void* Wp, int N,
                            int out_dtype, void* Y, void* ws, size_t ws_bytes, void* stream) {
     if (int rc = check_mx_types(format, out_dtype)) return rc;
     if (!codes || !scales || !Wp || !Y) return fail(DARD_ERR_ARG, "NULL pointer");
-    if (M < 1) return fail(DARD_ERR_SHAPE, "need M >= 1");
-    if (int rc = check_mx_weight(N, K)) return rc;
+    if (int rc = check_mx_product(M, N, K)) return rc;
     if (!aligned(codes, 16) || !aligned(Wp, 16)) return fail(DARD_ERR_ARG, "codes and Wp must be 16-byte aligned");
     if (!aligned(Y, esize(out_dtype))) return fail(DARD_ERR_ARG, "Y must be aligned to its element");
-    const size_t need = linear_mx_partial_bytes(format, M, N, K);
-    if (need && (!ws || ws_bytes < need)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", need);
-    if (need && !aligned(ws, 16)) return fail(DARD_ERR_ARG, "the workspace must be 16-byte aligned");
-    HIPOK(launch_linear_mx(format, (const uint8_t*)codes, scales, M, K, Wp, N, out_dtype, Y, (float*)ws,
-                           (hipStream_t)stream));
+    HIPOK(launch_linear_mx(format, (const uint8_t*)codes, scales, M, K, Wp, N, out_dtype, Y, (hipStream_t)stream));
     return DARD_OK;
 }
 

@@ -247,11 +247,9 @@ hipError_t launch_dequantize_mx(int format, const uint8_t* codes, const uint8_t*
 hipError_t launch_resid_norm_mx(float* h, int delta_dtype, const void* delta, int gain_dtype, const void* gain, float eps,
                                 int rows, int d, int format, uint8_t* codes, uint8_t* scales, hipStream_t s);
 hipError_t launch_pack_mx(const void* codes, const uint8_t* scales, int N, int K, void* Wp, hipStream_t s);
-// Y = X W^T (float32 or bf16 [M][N]); part: room for the partials of a K split
-// over workgroups, linear_mx_partial_bytes() of it.
-size_t linear_mx_partial_bytes(int format, int M, int N, int K);
+// Y = X W^T (float32 or bf16 [M][N]).
 hipError_t launch_linear_mx(int format, const uint8_t* xc, const uint8_t* xs, int M, int K, const void* Wp, int N,
-                            int out_dtype, void* y, float* part, hipStream_t s);
+                            int out_dtype, void* y, hipStream_t s);
 // The MXFP4 cache of one layer: K codes [b][Hkv][cap][dh/2], scales
 // [b][Hkv][cap][dh/32]; V in groups of 8 keys, codes
 // [b][Hkv][cap/8][dh/4][8][2], scales [b][Hkv][cap/8][dh/32][8].

@@ -229,6 +229,63 @@ def test_linear_error_norm(fmt, M, N, K):
     assert np.linalg.norm(got - ref) <= 1e-5 * np.linalg.norm(ref)
 
 
+# every kernel and both sides of its choice: rows per workgroup 32 to 256, K split over 1 to 8 groups of waves,
+# chunks of scales that are refilled, K that ends inside a unit
+CHOICES = [(1, 70, 1056), (1, 8230, 544), (1, 16520, 800), (33, 33010, 32), (33, 8230, 800), (1000, 12300, 32),
+           (1, 16520, 32), (100, 33010, 32), (5, 33010, 6240), (5, 16520, 12320), (5, 8230, 33056), (64, 520, 33056),
+           (40, 33010, 6240), (40, 8230, 33056), (100, 33010, 6240), (600, 8230, 4128), (2050, 4130, 2080), (1030, 33010, 288)]
+
+
+@pytest.mark.parametrize("M,N,K", CHOICES)
+def test_linear_exact_sums(M, N, K):
+    """Values whose products are small multiples of 1/16: their sums are exact in float32 in any order, and
+    within the bits that the matrix instructions keep."""
+    announce("linear exact sums", M, N, K)
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    def ints(hi, *shape):
+        return torch.randint(0, hi, shape, generator=g, device="cuda", dtype=torch.uint8)
+    e2m1 = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], device="cuda")
+    e4m3 = torch.tensor([0, 0x30, 0x38, 0x3C, 0x40, 0x80, 0xB0, 0xB8, 0xBC, 0xC0], device="cuda", dtype=torch.uint8)
+    v4m3 = torch.tensor([0, .5, 1, 1.5, 2, 0, -.5, -1, -1.5, -2], device="cuda")
+    def times(v, sc):
+        return v * torch.exp2(sc.float() - 127).repeat_interleave(32, 1)
+    wi, ws = ints(16, N, K), 126 + ints(3, N, K // 32)
+    wp = torch.empty(dard.dard_packed_mx_bytes(N, K), dtype=torch.uint8, device="cuda")
+    dard.dard_pack_matrix_mx(wi[:, ::2] | wi[:, 1::2] << 4, ws, wp)
+    w = times(e2m1[wi.long()], ws).double()
+    xs = 126 + ints(3, M, K // 32)
+    for fmt in FORMATS:
+        xi = ints(10 if fmt == R.FP8 else 16, M, K).long()
+        codes = e4m3[xi] if fmt == R.FP8 else (xi[:, ::2] | xi[:, 1::2] << 4).to(torch.uint8)
+        x = times((v4m3 if fmt == R.FP8 else e2m1)[xi], xs).double()
+        ref = x @ w.T
+        for out in (torch.float32, torch.bfloat16):
+            y = torch.full((M * N + 32,), 7.0, dtype=out, device="cuda")
+            dard.dard_linear_mx(fmt, codes, xs, wp, y[:M * N].view(M, N))
+            assert bool((y[M * N:] == 7.0).all())
+            assert torch.equal(y[:M * N].view(M, N), ref.to(torch.float32).to(out)), (fmt, out)
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 100, 4096), (40, 8230, 800), (300, 33010, 96)])
+def test_linear_high_scales_stay_local(M, N, K):
+    """Scale codes past those of quantised float32 in one row of x and one of w: their results are right, the
+    others keep their bits."""
+    announce("linear high scales", M, N, K)
+    xc, xs, _ = mx_rows(M, K, R.FP8, 1)
+    wc, ws, _ = mx_rows(N, K, R.FP4, 2)
+    xs[:, 0], ws[:, -1] = 40, 40
+    clean = run_linear(xc, xs, R.FP8, wc, ws, N, torch.float32).cpu().numpy()
+    m, n = M - 3, N - 5
+    xs[m, -1], ws[n, 0] = 250, 254   # (times 2^-87 of the others': in range)
+    got = run_linear(xc, xs, R.FP8, wc, ws, N, torch.float32).cpu().numpy()
+    rest = np.ones((M, N), bool)
+    rest[m], rest[:, n] = False, False
+    assert np.array_equal(got[rest], clean[rest])
+    x, w = R.values(xc, xs, R.FP8), R.values(wc, ws, R.FP4)
+    for a, b, y in ((x[m:m + 1], w, got[m:m + 1]), (x, w[n:n + 1], got[:, n:n + 1])):
+        assert np.all(np.abs(y.astype(np.float64) - a @ b.T) <= R.product_bound(a, b, scaled=True))
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("M,N,K", [(5, 70, 512), (70, 70, 288), (280, 300, 512)])
 def test_linear_nan_blocks(fmt, M, N, K):

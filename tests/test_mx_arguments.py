@@ -187,3 +187,11 @@ def test_reference_cache_layout():
         assert vs[s, h, key // 8, byte // 16, key % 8] == scales[s, h, key, byte // 16]
     c, sc = R.rows_of_cache(vc, vs)
     assert np.array_equal(c, codes) and np.array_equal(sc, scales)
+
+
+def test_size_limits():
+    L = dard.lib()
+    assert L.dard_packed_mx_bytes(1, (1 << 20) + 32) == 0 and L.dard_packed_mx_bytes(1, 1 << 20) > 0
+    assert L.dard_linear_mx(0, P, P, 1 << 30, 32, P, 1 << 20, 0, P, None, 0, None) == -2
+    assert L.dard_resid_norm_mx(P, 0, None, 0, P, 1e-5, 1 << 24, 32, 0, P, P, None) == -2
+    assert L.dard_quantize_mx(0, P, 32, 1 << 30, 32, 0, P, P, None) == -2
