@@ -4,12 +4,20 @@
 // Flash-style on v_mfma_f32_32x32x16_bf16: S^T = K Q^T and O^T += V^T P^T over
 // tiles of 32 keys, with a running maximum and sum per query row.  The rows of
 // all query heads of a KV head are one row space.  A wave takes 32 JT rows and
-// whole key tiles on its own: codes go from memory straight to its registers in
-// operand order and are widened to bf16 there by the scaled conversions (exact:
-// an E2M1 value times a power of two), so the main loop has no LDS traffic and
-// no barrier.  The four waves of a workgroup take interleaved tiles and merge
+// whole key tiles on its own: codes go from memory straight to its ring in LDS, in
+// operand order, and are widened to bf16 in registers by the scaled conversions
+// (exact: an E2M1 value times a power of two), so the main loop has no barrier.
+// The four waves of a workgroup take interleaved tiles and merge
 // through LDS; long key ranges are also split over workgroups (fp32 partials,
 // merged in split order by a second kernel).
+//
+// What bounds it: per tile and 64 rows 32 matrix instructions and about 250
+// others, of which 64 widen codes, 32 pair V's keys and 32 are exp2.  On random
+// data the matrix instructions alone run at 1.55 PFLOP/s (clocks fall under their
+// power) and a mix in these proportions, two waves a SIMD, takes 0.89 us a tile and
+// SIMD; the main loop takes 1.04.  Two waves a SIMD with the queries in LDS (read
+// anew for every tile) beat one wave with them in registers, 133 to 170 us at 448 rows
+// and 131136 keys, though that one alternates both kinds of instruction by hand.
 //
 // Operand order.  Lane l is row l % 32 of an operand, eta = l / 32.
 //   S^T: A row i holds key pi(i), pi swapping bits 2 and 3, and a lane's dims are
@@ -43,6 +51,12 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     typedef float f2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, bf16x2));
+}
+
+// s plus both values of a pair.
+__device__ __forceinline__ float add_pair(uint32_t pair, float s) {
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), one, s, false);
 }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -102,14 +116,17 @@ template <int DH> struct Tiles {
     }
     __device__ __forceinline__ void copy(int t, char* slot) const {
         const __amdgpu_buffer_rsrc_t k = rsrc(kc + (size_t)t * (16 * DH)), v = rsrc(vc + (size_t)t * (16 * DH));
+        const __amdgpu_buffer_rsrc_t sk = rsrc(ks + (size_t)t * DH), sv = rsrc(vs + (size_t)t * DH);
 #pragma unroll
         for (int i = 0; i < DH / 64; ++i) copy16_lds(k, slot + i * 1024, ko + 16 * i);
 #pragma unroll
         for (int i = 0; i < DH / 64; ++i) copy16_lds(v, slot + Slot<DH>::kV + i * 1024, vo + 1024 * i);
-        if (scales) {
-            copy16_lds(rsrc(ks + (size_t)t * DH), slot + Slot<DH>::kKs, vs16);
-            copy16_lds(rsrc(vs + (size_t)t * DH), slot + Slot<DH>::kVs, vs16);
+        __builtin_amdgcn_sched_barrier(0);
+        if (scales) {   // (nothing else in here: without a branch around them the compiler's own counts of copies hold)
+            copy16_lds(sk, slot + Slot<DH>::kKs, vs16);
+            copy16_lds(sv, slot + Slot<DH>::kVs, vs16);
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
 };
 
@@ -187,9 +204,9 @@ __device__ __forceinline__ void probabilities(const floatx16 (&st)[JT], float c,
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p0 = exp2_fast(fmaf(st[jt][2 * e], c, -m[jt])), p1 = exp2_fast(fmaf(st[jt][2 * e + 1], c, -m[jt]));
-            a += p0;
-            b += p1;
             p[jt][e] = pack_bf16(p0, p1);
+            if (e & 1) b = add_pair(p[jt][e], b);
+            else a = add_pair(p[jt][e], a);
         }
         sum[jt] = a + b;
     };
@@ -266,9 +283,10 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
     constexpr int kMerge = NT * 4 * 64 * 16;           // O of one row tile of a wave
     // One array (several would carry alias information by which the compiler makes every LDS read
     // wait for every copy in flight): the rings and the query operands, in whose place O of one row
-    // tile of the four waves lies at the end; the waves' maxima and sums; the rows' take-x words and their complements; the
-    // rows' visibility strings.
-    constexpr int kQ = 4 * kRing, kMl = kQ + JT * NJ * 1024 > 4 * kMerge ? kQ + JT * NJ * 1024 : 4 * kMerge, kXs = kMl + 4 * JT * 64 * 4, kVis = kXs + 32 * JT * 2 * kBlockWords * 8;
+    // tile of the four waves lies at the end; the waves' maxima and sums; the rows' take-x words and their
+    // complements; the rows' visibility strings.
+    constexpr int kQ = 4 * kRing, kMl = kQ + JT * NJ * 1024 > 4 * kMerge ? kQ + JT * NJ * 1024 : 4 * kMerge;
+    constexpr int kXs = kMl + 4 * JT * 64 * 4, kVis = kXs + 32 * JT * 2 * kBlockWords * 8;
     __shared__ __attribute__((aligned(16))) char smem[kVis + 32 * JT * kVisWords * 4];
     float* const ml = reinterpret_cast<float*>(smem + kMl);
     uint64_t* const xs = reinterpret_cast<uint64_t*>(smem + kXs);
@@ -327,10 +345,9 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
     const int full = max(0, (min(t1, P / kTileKeys) - first + 3) >> 2);
     int at = 0;            // ring slot of tile i
     auto next_slot = [&](int x) { return x + 1 == kDepth ? 0 : x + 1; };
-    if (n > 0) {
 #pragma unroll
-        for (int i = 0; i < kDepth; ++i) tiles.copy(first + 4 * min(i, n - 1), ring + i * Slot<DH>::kBytes);
-    }
+    for (int i = 0; i < kDepth; ++i)
+        tiles.copy(min(first + 4 * min(i, max(n - 1, 0)), ntiles - 1), ring + i * Slot<DH>::kBytes);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < JT * NJ / 4; ++i) q[(4 * i + wave) * 64 + lane] = qv[i];
