@@ -567,7 +567,9 @@ int check_mx_attention(int b, int B, int Hq, int Hkv, int dh, int P) {
     if (b < 1 || B < 1 || B > 256 || P < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || P > 0x7FFFFFFF - 1024)
         return fail(DARD_ERR_SHAPE, "bad attention shape (b=%d B=%d P=%d Hq=%d Hkv=%d)", b, B, P, Hq, Hkv);
     if (dh != 64 && dh != 128) return fail(DARD_ERR_SHAPE, "dh must be 64 or 128");
-    if ((double)b * 2 * B * Hq * (dh / 4) > 2147483647.0) return fail(DARD_ERR_SHAPE, "too many query rows in one call");
+    // (threads of a grid are counted in 32 bits: of the merge, and of a workgroup per 32 rows of a KV head)
+    if ((double)b * 2 * B * Hq * (dh / 4) > 2147483647.0 || (double)b * Hkv * ((Hq / Hkv * 2 * B + 31) / 32) >= 16777216.0)
+        return fail(DARD_ERR_SHAPE, "too many query rows in one call");
     return DARD_OK;
 }
 
@@ -582,6 +584,7 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
                                      int b, int B, int Hq, int Hkv, int dh, float scale, uint32_t flags, void* out,
                                      void* ws, size_t ws_bytes, void* stream) {
     if (!q || !state || !conf || !out) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (!(scale > 0.f && scale < INFINITY)) return fail(DARD_ERR_ARG, "need a finite scale > 0");
     if (int rc = check_flags(flags)) return rc;
     if (int rc = check_mx_attention(b, B, Hq, Hkv, dh, P)) return rc;
     if (int rc = check_mx_cache(kc, ks, vc, vs, b, Hkv, dh, cap)) return rc;

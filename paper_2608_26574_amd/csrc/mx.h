@@ -16,12 +16,12 @@ constexpr int kMxBlock = 32;
 
 template <int F> struct Mx;   // element format
 template <> struct Mx<DARD_MX_FP8> {
-    static constexpr int kEmax = 8, kBits = 8, kMant = 3, kEmin = -6;
+    static constexpr int kEmax = 8, kMant = 3, kEmin = -6;
     static constexpr float kTop = 448.f;
     static constexpr int kMfma = 0;   // operand format code of the scaled matrix instructions
 };
 template <> struct Mx<DARD_MX_FP4> {
-    static constexpr int kEmax = 2, kBits = 4, kMant = 1, kEmin = 0;
+    static constexpr int kEmax = 2, kMant = 1, kEmin = 0;
     static constexpr float kTop = 6.f;
     static constexpr int kMfma = 4;
 };
@@ -85,9 +85,6 @@ template <int F> __device__ __forceinline__ float mx_value(uint32_t c) {
         return __uint_as_float((uint32_t)fp4x2_to_bf16x2<0>(c & 15u, 1.0f) << 16);
     }
 }
-
-// Loads of 8 or 16 bytes at any address (rows whose length is not a multiple).
-struct __attribute__((packed, aligned(1))) Bytes8 { uint32_t x, y; };
 
 // Eight consecutive values as floats; p only as aligned as its element.
 __device__ __forceinline__ void ld_8(const float* p, float (&v)[8]) {

@@ -195,3 +195,8 @@ def test_size_limits():
     assert L.dard_linear_mx(0, P, P, 1 << 30, 32, P, 1 << 20, 0, P, None, 0, None) == -2
     assert L.dard_resid_norm_mx(P, 0, None, 0, P, 1e-5, 1 << 24, 32, 0, P, P, None) == -2
     assert L.dard_quantize_mx(0, P, 32, 1 << 30, 32, 0, P, P, None) == -2
+    f = lambda b, scale: L.dard_masked_attention_mx(   # noqa: E731
+        P, P, P, P, P, 10, None, 64, P, P, b, 1, 4, 4, 128, scale, 0, P, P, BIG, None)
+    assert f(1 << 22, 0.1) == -2   # 2^24 workgroups
+    for scale in (0.0, -0.1, float("inf"), float("nan")):
+        assert f(1, scale) == -1
