@@ -32,6 +32,8 @@
 // Key tiles are aligned to 32 from key 0.  Tiles below the sequence's prefix
 // length are seen by every row; later ones are tested against the row's
 // visibility string (one bit per block key, x then s; zero past the block).
+#include <cmath>
+
 #include "launch.h"
 #include "mx.h"
 
@@ -553,25 +555,48 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
     }
 }
 
-// Merge of the key splits, in split order: a thread takes 4 dims of a row.
+// Merge of the key splits.  DH / 4 lanes take a row, 4 dims each; lane g also fetches the maximum and sum of
+// split g (g + DH / 4, ...) for all of them, so that a row costs two dependent reads
+// and not two per split: the reads of a row's partial results go out eight at a time.
 template <int DH>
 __global__ __launch_bounds__(256) void attn_mx_combine_kernel(const float* __restrict__ part, int nsplit, int64_t rows,
                                                               bf16_t* __restrict__ out) {
+    constexpr int G = DH / 4;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * (DH / 4)) return;
-    const int64_t row = i / (DH / 4);
-    const float* ml = part + nsplit * rows * DH;
+    const int g = threadIdx.x % G;
+    const int64_t row = i / G < rows ? i / G : rows - 1;   // (every lane takes part in the exchanges)
+    const float* ml = part + nsplit * rows * DH + 2 * row;
+    const floatx4* px = reinterpret_cast<const floatx4*>(part + row * DH) + g;
     float mm = kFloor;
-    for (int s = 0; s < nsplit; ++s) mm = fmaxf(mm, ml[(s * rows + row) * 2]);
+    for (int s = g; s < nsplit; s += G) mm = fmaxf(mm, ml[2 * s * rows]);
+#pragma unroll
+    for (int d = G / 2; d > 0; d /= 2) mm = fmaxf(mm, __shfl_xor(mm, d, 64));
     floatx4 x = floatx4{};
     float l = 0.f;
-    for (int s = 0; s < nsplit; ++s) {
-        const float f = exp2_fast(ml[(s * rows + row) * 2] - mm);
-        l += ml[(s * rows + row) * 2 + 1] * f;
-        x += reinterpret_cast<const floatx4*>(part)[s * rows * (DH / 4) + i] * f;
+    for (int s0 = 0; s0 < nsplit; s0 += G) {
+        const int s = s0 + g;
+        float f = 0.f;
+        if (s < nsplit) {
+            f = exp2_fast(ml[2 * s * rows] - mm);
+            l += ml[2 * s * rows + 1] * f;
+        }
+        const int n = min(G, nsplit - s0);
+        for (int k = 0; k < n; k += 8) {
+            floatx4 t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = px[min(s0 + k + e, nsplit - 1) * rows * G];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float w = __shfl(f, (k + e) % G, G);   // (0 past the last split)
+                if (k + e < n) x += t[e] * w;
+            }
+        }
     }
+#pragma unroll
+    for (int d = G / 2; d > 0; d /= 2) l += __shfl_xor(l, d, 64);
     const float inv = 1.f / l;
-    reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
+    if (i / G < rows)
+        reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
 constexpr int kSlots = 512;   // workgroups at once: two on each of 256 CUs
@@ -580,19 +605,34 @@ struct Plan {
     int jt, rowtiles, split, tps;
 };
 
-Plan plan_of(int b, int B, int Hq, int Hkv, int P) {
+// Keys are split over the workgroups when that is cheaper than the merge.  Costs in us, fitted to a sweep of splits
+// 1 to 32 over 3 head layouts, 1 to 8 sequences, blocks of 1 to 64 and prefixes of 60 to 40000 (the
+// split of least cost loses 0.4% to the best): a tile of a wave costs `alone` when its workgroup has a CU to
+// itself and `shared` when two share one; a full chip starts 2.6 later than an empty one, a further
+// round of workgroups 2.7; the merge takes 2.5, 0.05 a split and 0.2 a megabyte of partial results.
+Plan plan_of(int b, int B, int Hq, int Hkv, int dh, int P) {
     Plan p;
     const int nrows = Hq / Hkv * 2 * B;
     p.jt = nrows > 32 ? 2 : 1;
     p.rowtiles = (nrows + 32 * p.jt - 1) / (32 * p.jt);
     const int ntiles = (P + 2 * B + kTileKeys - 1) / kTileKeys;
-    const int64_t wgs = (int64_t)p.rowtiles * Hkv * b;
-    // one round of workgroups, two tiles a wave at least
-    const int64_t room = kSlots / wgs;
-    const int most = (ntiles + 7) / 8;
-    p.split = (int)(room < most ? (room > 1 ? room : 1) : most);
-    p.tps = (ntiles + p.split - 1) / p.split;
-    p.split = (ntiles + p.tps - 1) / p.tps;
+    const double wgs = (double)p.rowtiles * Hkv * b, mb = 8e-6 * b * 2 * B * Hq * dh;
+    const double alone = p.jt == 2 ? (dh == 128 ? 1.0 : 0.78) : dh == 128 ? 0.65 : 0.51;
+    const double shared = p.jt == 2 ? (dh == 128 ? 1.77 : 1.44) : dh == 128 ? 1.18 : 0.96;
+    static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+    double best = 1e300;
+    for (int split : kSplits) {
+        const int tps = (ntiles + split - 1) / split, n = (ntiles + tps - 1) / tps;
+        const double all = wgs * n, rounds = std::ceil(all / kSlots);
+        double cost = (tps + 3) / 4 * rounds * (all <= kSlots / 2 ? alone : shared) + 2.7 * (rounds - 1) +
+                      2.6 * (all < kSlots ? all / kSlots : 1.0);
+        if (n > 1) cost += 2.5 + 0.05 * n + mb * n * 0.2;
+        if (cost < best) {
+            best = cost;
+            p.split = n;
+            p.tps = tps;
+        }
+    }
     return p;
 }
 
@@ -603,12 +643,12 @@ template <int DH, int JT> void run(const MxAttnArgs& a, const Plan& p, hipStream
 }  // namespace
 
 size_t attention_mx_partial_bytes(int b, int B, int Hq, int Hkv, int dh, int P) {
-    const Plan p = plan_of(b, B, Hq, Hkv, P);
+    const Plan p = plan_of(b, B, Hq, Hkv, dh, P);
     return p.split > 1 ? (size_t)p.split * b * 2 * B * Hq * (dh + 2) * 4 : 0;
 }
 
 hipError_t launch_attention_mx(const MxAttnArgs& a, hipStream_t s) {
-    const Plan p = plan_of(a.b, a.B, a.Hq, a.Hkv, a.P);
+    const Plan p = plan_of(a.b, a.B, a.Hq, a.Hkv, a.dh, a.P);
     if (a.dh == 128) {
         if (p.jt == 2) run<128, 2>(a, p, s);
         else run<128, 1>(a, p, s);
