@@ -199,6 +199,14 @@ def test_attention_long(B, P, Hq, Hkv, dh):
     attention_case(1, B, P, Hq, Hkv, dh, seed=5)
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+def test_attention_many_splits(dh):
+    """Keys split over some 90 workgroups (more than the lanes that merge a row), most of them empty for the
+    shorter sequences."""
+    announce("attention mx many splits", dh)
+    attention_case(3, 2, 100000, 1, 1, dh, lens=[100000, 5, 33000], seed=6)
+
+
 def test_attention_peaked():
     """Scores far apart: the running maximum moves, and most probabilities vanish."""
     announce("attention mx peaked")
