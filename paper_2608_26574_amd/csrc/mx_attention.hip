@@ -382,11 +382,12 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
         }
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
         wg_barrier();
-        // bit j of a row's string: key j of the block, x keys (bits of x), then s keys (the others)
-        for (int i = threadIdx.x; i < 32 * JT * kVisWords / 2; i += 256) {
-            const uint64_t* w = xs + i / (kVisWords / 2) * 2 * kBlockWords;
-            const int start = 64 * (i % (kVisWords / 2));
-            vis[i] = bits_at(w, start) | bits_at(w + kBlockWords, start - a.B);
+        // bit j of a row's string: key j of the block, x keys (bits of x), then s keys (the others).  The
+        // words that tiles up to the block's end read: the last one from bit 2 B - 1 at most.
+        for (int i = threadIdx.x; i < 32 * JT * ((2 * a.B + 31) / 64 + 1); i += 256) {
+            const int at = i % (32 * JT), word = i / (32 * JT), start = 64 * word;
+            const uint64_t* w = xs + at * 2 * kBlockWords;
+            vis[at * (kVisWords / 2) + word] = bits_at(w, start) | bits_at(w + kBlockWords, start - a.B);
         }
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
