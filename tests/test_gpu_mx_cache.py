@@ -111,8 +111,9 @@ def visible(state, conf, P, flags):
 def attend(q, k, v, seen, scale):
     """(out, its largest error) of one head: q [R][dh], k, v [K][dh].
 
-    Probabilities are rounded to bf16 (2^-8 of each, while their sum is taken
-    before), and so is the output.  A score is a float32 sum of dh products,
+    Probabilities are rounded to bf16 (2^-8 of each, which moves the weighted
+    sum of values and the sum of them that divides it by at most 2^-8 of their
+    size each), and so is the output: 3 times 2^-8.  A score is a float32 sum of dh products,
     off by at most dh 2^-23 sum |q k|, scaled and shifted (a few roundings of
     it more), and exp2 is good to 2^-20; each of these moves a probability and the
     sum it is divided by."""
@@ -121,7 +122,7 @@ def attend(q, k, v, seen, scale):
     p = np.exp(s - s.max(-1, keepdims=True))
     p /= p.sum(-1, keepdims=True)
     off = (q.shape[1] + 8) * 2.0 ** -23 * (np.abs(q) @ np.abs(k).T).max(-1, keepdims=True) * scale + 2.0 ** -20
-    return p @ v, (2.0 ** -7 + 2 * off) * (p @ np.abs(v)) + 1e-30
+    return p @ v, (3 * 2.0 ** -8 + 2 * off) * (p @ np.abs(v)) + 1e-30
 
 
 def attention_case(b, B, P, Hq, Hkv, dh, flags=0, lens=None, seed=0, cap_extra=0, qstd=1.0, nan_key=None):
