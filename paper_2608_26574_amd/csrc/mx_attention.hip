@@ -1,7 +1,7 @@
 // State-masked attention over an MXFP4 key/value cache (Sec. 3.1, Sec. 3.2;
 // the block-scaled form of the prefix cache of App. C.5).
 //
-// Flash-style on v_mfma_f32_32x32x16_bf16: S^T = K Q^T and O^T += V^T P^T over
+// One pass over the keys on v_mfma_f32_32x32x16_bf16: S^T = K Q^T and O^T += V^T P^T over
 // tiles of 32 keys, with a running maximum and sum per query row.  The rows of
 // all query heads of a KV head are one row space.  A wave takes 32 JT rows and
 // whole key tiles on its own: codes go from memory straight to its ring in LDS, in

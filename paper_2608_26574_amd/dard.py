@@ -293,22 +293,26 @@ def _args(stream, tensors, strided=()):
         if t is None:
             ptrs.append(None)
             continue
+        d = t.get_device()
+        if d != dev or d < 0:
+            _wrong_device(d, dev)
         if not t.is_contiguous():
             raise ValueError("libdard takes contiguous tensors")
-        ptrs.append(t)
-    ptrs += strided
-    for i, t in enumerate(ptrs):
-        if t is None:
-            continue
+        ptrs.append(t.data_ptr())
+    for t in strided:
         d = t.get_device()
-        if d < 0:
-            raise ValueError("libdard takes device tensors")
-        if d != dev:
-            raise ValueError(f"tensor on cuda:{d}, but the current device is cuda:{dev}")
-        ptrs[i] = t.data_ptr()
+        if d != dev or d < 0:
+            _wrong_device(d, dev)
+        ptrs.append(t.data_ptr())
     if stream is None:
         return ptrs, torch._C._cuda_getCurrentRawStream(dev)
     return ptrs, _stream(stream)
+
+
+def _wrong_device(d, dev):
+    if d < 0:
+        raise ValueError("libdard takes device tensors")
+    raise ValueError(f"tensor on cuda:{d}, but the current device is cuda:{dev}")
 
 
 def _rows_ld(t, what):
@@ -385,7 +389,7 @@ def dard_linear_mx(format, codes, scales, Wp, Y, ws=None, stream=None):
     M, N = Y.shape
     K = codes.shape[1] * (1 if format == MX_FP8 else 2)
     _mx_check(M, K, format, codes, scales)
-    if _nbytes(Wp) < dard_packed_mx_bytes(N, K):
+    if _nbytes(Wp) < -(-N // 32) * -(-K // 256) * 4352:   # (dard_packed_mx_bytes: 32 x 256 values a block, 17 bytes for 32)
         raise ValueError(f"Wp of {_nbytes(Wp)} bytes does not hold a packed [{N}][{K}] matrix")
     dt = _mx_dt(Y, "Y")
     (c, s, w, y, room), st = _args(stream, (codes, scales, Wp, Y, ws))
@@ -395,14 +399,17 @@ def dard_linear_mx(format, codes, scales, Wp, Y, ws=None, stream=None):
 def _mx_cache(cache, b, Hkv, dh):
     """Capacity of an MXFP4 cache (kc, ks, vc, vs) of b sequences."""
     kc, ks, vc, vs = cache
-    if kc.dim() != 4:
+    shape = kc.shape
+    if len(shape) != 4:
         raise ValueError("kc must be [b][Hkv][cap][dh/2]")
-    cap = kc.shape[2]
+    cap, u8 = shape[2], torch.uint8
     want = ((b, Hkv, cap, dh // 2), (b, Hkv, cap, dh // 32), (b, Hkv, cap // 8, dh // 4, 8, 2),
             (b, Hkv, cap // 8, dh // 32, 8))
-    for name, t, shape in zip(("kc", "ks", "vc", "vs"), cache, want):
-        if t.shape != shape or t.dtype is not torch.uint8:
-            raise ValueError(f"{name} must be uint8 {shape}, got {t.dtype} {tuple(t.shape)}")
+    if not (shape == want[0] and ks.shape == want[1] and vc.shape == want[2] and vs.shape == want[3] and kc.dtype is u8
+            and ks.dtype is u8 and vc.dtype is u8 and vs.dtype is u8):
+        for name, t, w in zip(("kc", "ks", "vc", "vs"), cache, want):
+            if t.shape != w or t.dtype is not u8:
+                raise ValueError(f"{name} must be uint8 {w}, got {t.dtype} {tuple(t.shape)}")
     return cap
 
 
@@ -412,10 +419,10 @@ def _mx_prefix(prefix, b):
     return prefix
 
 
-def _tokens_ld(t, what):
+def _tokens_ld(shape, stride, what):
     """Elements between the tokens of a [b][n][Hkv][dh] tensor whose heads are contiguous."""
-    b, n, Hkv, dh = t.shape
-    sb, sn, sh, sd = t.stride()
+    b, n, Hkv, dh = shape
+    sb, sn, sh, sd = stride
     ld = sn if n > 1 else (sb if b > 1 else Hkv * dh)
     if (dh > 1 and sd != 1) or (Hkv > 1 and sh != dh) or (b > 1 and sb != n * ld):
         raise ValueError(f"{what} must be [b][n][Hkv][dh] with contiguous heads and evenly spaced tokens")
@@ -423,12 +430,14 @@ def _tokens_ld(t, what):
 
 
 def _kv_args(cache, k, v, prefix, stream):
-    if k.shape != v.shape or k.dtype is not v.dtype or k.dim() != 4:
+    shape = k.shape
+    if v.shape != shape or k.dtype is not v.dtype or len(shape) != 4:
         raise ValueError("k and v must be [b][n][Hkv][dh] tensors of one type")
-    b, n, Hkv, dh = k.shape
+    b, n, Hkv, dh = shape
     cap = _mx_cache(cache, b, Hkv, dh)
-    ld = _tokens_ld(k, "k")
-    if _tokens_ld(v, "v") != ld:
+    stride, other = k.stride(), v.stride()
+    ld = _tokens_ld(shape, stride, "k")
+    if other != stride and _tokens_ld(shape, other, "v") != ld:
         raise ValueError("k and v must have the same distance between tokens")
     dt = _mx_dt(k, "k")
     ptrs, st = _args(stream, (*cache, _mx_prefix(prefix, b)), (k, v))

@@ -302,6 +302,22 @@ def test_linear_nan_blocks(fmt, M, N, K):
     assert np.array_equal(got[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("M,N,K", [(5, 70, 512), (40, 8230, 288), (300, 33010, 96)])
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_linear_nan_codes(M, N, K, out):
+    """An E4M3 NaN code makes its row NaN and nothing else."""
+    announce("linear nan codes", M, N, K, out)
+    xc, xs, _ = mx_rows(M, K, R.FP8, 1)
+    wc, ws, _ = mx_rows(N, K, R.FP4, 2)
+    clean = run_linear(xc, xs, R.FP8, wc, ws, N, out)
+    xc[M - 2, K - 1], xc[0, 3] = 0x7F, 0xFF
+    got = run_linear(xc, xs, R.FP8, wc, ws, N, out)
+    rest = torch.ones(M, dtype=torch.bool)
+    rest[[0, M - 2]] = False
+    assert bool(torch.isnan(got[~rest]).all())
+    assert torch.equal(got[rest], clean[rest])
+
+
 def test_linear_scale_extremes():
     announce("linear scale extremes")
     M, N, K = 4, 32, 64
