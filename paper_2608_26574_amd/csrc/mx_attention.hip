@@ -420,7 +420,12 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
         uint32_t p[JT][8];
         scores<DH, JT>(k, q, lane, st);
         probabilities<JT, NT>(st, c, m, l, o, p);
+        // the wave that has its probabilities goes first: its matrix instructions run under the other
+        // wave's vector ones (448 rows, 131136 keys: 135 -> 130 us; first with the scores too 133, with the
+        // probabilities 136)
+        __builtin_amdgcn_s_setprio(1);
         add_values<DH, JT>(v, p, lr, o);
+        __builtin_amdgcn_s_setprio(0);
         refill(i);
     }
     // tiles at the prefix's end and in the block
