@@ -222,10 +222,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_xs(const LinArgs& a, int 
 // Merge of the K groups of the few-rows kernels through LDS, and stores: element 4 q + c of a block is
 // row 8 q + 4 eta + c, column lane % 32.
 // mend(the wave's part): what may be put right in between.
-template <int TI, int KG, typename Mend>
+template <int TI, int NW, int KG, typename Mend>
 __device__ __forceinline__ void merge_rows(const LinArgs& a, const floatx16 (&acc)[TI], floatx4* red, int m0, int n0, int wave,
                                            int lane, Mend&& mend) {
-    constexpr int CW = 8 / KG;
+    constexpr int CW = NW / KG;
     const int lr = lane & 31, eta = lane >> 5;
 #pragma unroll
     for (int i = 0; i < TI; ++i)
@@ -236,7 +236,7 @@ __device__ __forceinline__ void merge_rows(const LinArgs& a, const floatx16 (&ac
     mend(red + wave * TI * 256);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
     wg_barrier();
-    for (int t = wave; t < CW * TI * 4; t += 8) {
+    for (int t = wave; t < CW * TI * 4; t += NW) {
         const int q = t & 3, i = (t >> 2) % TI, c2 = (t >> 2) / TI;
         floatx4 v = floatx4{};
 #pragma unroll
@@ -250,28 +250,29 @@ __device__ __forceinline__ void merge_rows(const LinArgs& a, const floatx16 (&ac
 }
 
 // ---------------------------------------------------------------- few rows
-// Up to some hundred rows (see kKinds).  A workgroup of
-// eight waves makes 32 TI rows x 32 CW columns: CW = 8 / KG column waves of 32 columns, for
+// Up to some hundred rows (see kKinds).  A workgroup of NW (8 or 16)
+// waves makes 32 TI rows x 32 CW columns: CW = NW / KG column waves of 32 columns, for
 // each of KG groups that split the K units and merge through LDS at the end (so that a
 // narrow matrix keeps enough loads in flight without partial results in memory).  A wave's
 // weights and their scales go from memory straight to registers, rows of x through LDS, shared
 // by the column waves of a group; both D units (256 k) deep.
 // With few rows bound by the weights: 32 x 126464 x 4096 takes 53 us, 5.2 TB/s of weights, one row x 4096 x
 // 4096 6.6 (latency: 16 units of a wave's serial loads).  With more, by the widening next to
-// the matrix instructions: exact, 64 x 24576 x 4096 19.4 us (0.66 PFLOP/s on 192 CUs), 1024 x 3584 x
+// the matrix instructions: exact, 64 x 24576 x 4096 17.5 us (0.74 PFLOP/s on 192 CUs), 1024 x 3584 x
 // 18944 125 us (1.11 PFLOP/s); to bf16 14.5 and 70 us.
-template <int F, bool EX, int TI, int KG, int D, int OCC>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+template <int F, bool EX, int TI, int NW, int KG, int D, int OCC>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void linear_mx_rows_kernel(LinArgs a, int tiles_m) {
     constexpr bool F8 = F == DARD_MX_FP8;
-    constexpr int CW = 8 / KG, BM = 32 * TI, RB = F8 ? 256 : 128, CPR = RB / 16, RSH = F8 ? 0 : 1;
+    constexpr int CW = NW / KG, BM = 32 * TI, RB = F8 ? 256 : 128, CPR = RB / 16, RSH = F8 ? 0 : 1;
     constexpr int XB = BM * RB, NX = XB / 1024, CX = NX >= CW ? NX / CW : 1;   // 1 KB copies per unit: all, per wave
     constexpr int LW = 5;                                                     // register loads of a wave per unit
     // scales of x: chunks of CH units per group in LDS, as aligned dwords (two a unit and one more a row)
     constexpr int CH = D == 3 ? 12 : KG * TI >= 4 ? 8 : 16, SP = 2 * CH + 1, NSC = (BM * SP + CW * 64 - 1) / (CW * 64);
+    static_assert(NX % CX == 0, "whole copies per wave");
     static_assert(CH % D == 0 && CH > D, "chunks end with the unrolled loop's rounds");
     static_assert(D >= 2 && (D - 1) * (CX + LW) <= 63, "vmcnt range");
-    constexpr int RING = KG * D * XB, MERGE = 8 * TI * 4096, ALL = RING + KG * BM * SP * 4;
+    constexpr int RING = KG * D * XB, MERGE = NW * TI * 4096, ALL = RING + KG * BM * SP * 4;
     __shared__ __attribute__((aligned(16))) char smem[ALL > MERGE ? ALL : MERGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int cw = wave % CW, kg = wave / CW, lr = lane & 31, eta = lane >> 5;
@@ -326,7 +327,7 @@ void linear_mx_rows_kernel(LinArgs a, int tiles_m) {
     auto issue = [&](int i, Regs& r, int slot) __attribute__((always_inline)) {   // unit i of the group (past the last: repeated)
         const int u = u0 + (nu > 0 ? min(i, nu - 1) : 0), kb = u * RB;
         __builtin_amdgcn_sched_barrier(0);
-        if (NX >= CW || cw < NX) {
+        if (NX == CW * CX || cw < NX / CX) {
 #pragma unroll
             for (int j = 0; j < CX; ++j)
                 copy_lds<16>(rx, ring + slot * XB + (cw * CX + j) * 1024,
@@ -413,7 +414,7 @@ void linear_mx_rows_kernel(LinArgs a, int tiles_m) {
     floatx16 sum[TI];
 #pragma unroll
     for (int i = 0; i < TI; ++i) sum[i] = acc[i][0];
-    merge_rows<TI, KG>(a, sum, reinterpret_cast<floatx4*>(smem), m0, n0, wave, lane, [&](floatx4* red) __attribute__((always_inline)) {
+    merge_rows<TI, NW, KG>(a, sum, reinterpret_cast<floatx4*>(smem), m0, n0, wave, lane, [&](floatx4* red) __attribute__((always_inline)) {
         if constexpr (EX) {
             if (!__any((high.x | high.w) != 0)) return;
 #pragma unroll 1
@@ -640,22 +641,22 @@ void linear_mx_tile_kernel(LinArgs a, int tiles_m, int tiles_n) {
 }
 
 // A kernel with its tile, and what it costs (us): a round of 256 workgroups takes fixed + unit per 256 k of
-// a workgroup's K range.  Fitted to a sweep of all kernels over M 1 to 8192, N 3584 to 126464 and K
-// 512 to 18944 (the choice by cost loses 1% to the best kernel of each of its sizes); columns:
-// exact, MXFP8, MXFP4.
+// a workgroup's K range.  Fitted to a sweep of all kernels (and four that hardly pay: 32 x 128 and 64 x 64 in
+// eight waves, 32 x 192 in twelve, 64 x 256 in sixteen) over M 1 to 4096, N 3584 to 126464 and K 512 to 18944; the
+// choice by cost loses 2% to the best of all twelve for each size.  Columns: exact, MXFP8, MXFP4.
 struct Kind {
-    int rows, cols, kg;
+    int rows, cols, kg, threads;
     float fixed[3], unit[3];
 };
 constexpr Kind kKinds[] = {
-    {32, 256, 1, {3.6f, 3.7f, 1.8f}, {0.89f, 0.47f, 0.47f}},
-    {32, 128, 2, {4.3f, 3.8f, 2.2f}, {1.05f, 0.58f, 0.59f}},
-    {32, 64, 4, {3.9f, 3.3f, 2.1f}, {1.20f, 0.80f, 0.73f}},
-    {32, 32, 8, {2.7f, 2.2f, 1.8f}, {1.58f, 1.41f, 1.11f}},
-    {64, 256, 1, {4.8f, 5.0f, 3.8f}, {1.54f, 0.72f, 0.64f}},
-    {64, 64, 4, {3.8f, 3.1f, 2.2f}, {2.02f, 1.39f, 1.16f}},
-    {128, 256, 1, {8.6f, 8.0f, 9.8f}, {2.71f, 1.46f, 1.05f}},
-    {256, 256, 0, {9.4f, 7.8f, 11.3f}, {5.12f, 2.99f, 2.11f}},   // the tiled kernel
+    {32, 256, 1, 512, {3.4f, 3.9f, 2.4f}, {0.91f, 0.47f, 0.49f}},
+    {32, 128, 4, 1024, {3.2f, 3.4f, 2.8f}, {1.92f, 1.14f, 1.25f}},
+    {32, 64, 4, 512, {3.7f, 3.6f, 3.9f}, {1.25f, 0.77f, 0.63f}},
+    {32, 32, 8, 512, {3.2f, 3.6f, 4.5f}, {1.45f, 1.15f, 0.82f}},
+    {64, 256, 1, 512, {5.1f, 4.8f, 2.9f}, {1.54f, 0.75f, 0.69f}},
+    {64, 128, 4, 1024, {4.1f, 4.3f, 2.9f}, {3.23f, 1.73f, 1.60f}},
+    {128, 256, 1, 512, {8.7f, 8.4f, 10.3f}, {3.03f, 1.59f, 1.11f}},
+    {256, 256, 0, 256, {8.8f, 7.2f, 11.1f}, {5.58f, 3.34f, 2.16f}},   // the tiled kernel
 };
 
 int kind_of(int column, int M, int N, int K) {
@@ -665,7 +666,7 @@ int kind_of(int column, int M, int N, int K) {
     for (int i = 0; i < (int)(sizeof kKinds / sizeof kKinds[0]); ++i) {
         const Kind& k = kKinds[i];
         const double groups = std::ceil((double)M / k.rows) * std::ceil((double)N / k.cols);
-        if (groups >= 1 << 23 && k.kg) continue;                 // (a grid's threads are counted in 32 bits)
+        if (groups >= 1 << 22 && k.kg) continue;                 // (a grid's threads are counted in 32 bits)
         double cost = std::ceil(groups / 256) * (k.fixed[column] + std::ceil(units / (k.kg ? k.kg : 1)) * k.unit[column]);
         const double mem = (double)N * K * (17. / 32) / 3.5e6;   // (the weights' time, us)
         if (cost < mem) cost = mem + 1e-3 * cost;                // (a tie there: the least work)
@@ -682,15 +683,15 @@ template <int F, bool EX> void run(const LinArgs& a, hipStream_t s) {
     const Kind& k = kKinds[kind];
     const int tm = (a.M + k.rows - 1) / k.rows, tn = (a.N + k.cols - 1) / k.cols;
     const dim3 g((unsigned)tm * tn);
-    auto few = [&](auto kernel) { launch(kernel, g, dim3(512), 0, s, a, tm); };
+    auto few = [&](auto kernel) { launch(kernel, g, dim3(k.threads), 0, s, a, tm); };
     switch (kind) {
-        case 0: few(linear_mx_rows_kernel<F, EX, 1, 1, EX ? 2 : 3, 4>); break;   // (depths: what the registers hold)
-        case 1: few(linear_mx_rows_kernel<F, EX, 1, 2, 4, 2>); break;
-        case 2: few(linear_mx_rows_kernel<F, EX, 1, 4, 4, 2>); break;
-        case 3: few(linear_mx_rows_kernel<F, EX, 1, 8, 2, 2>); break;
-        case 4: few(linear_mx_rows_kernel<F, EX, 2, 1, F == DARD_MX_FP8 ? 2 : 3, 4>); break;
-        case 5: few(linear_mx_rows_kernel<F, EX, 2, 4, 2, 2>); break;
-        case 6: few(linear_mx_rows_kernel<F, EX, 4, 1, 3, 2>); break;
+        case 0: few(linear_mx_rows_kernel<F, EX, 1, 8, 1, EX ? 2 : 3, 4>); break;   // (depths: what the registers hold)
+        case 1: few(linear_mx_rows_kernel<F, EX, 1, 16, 4, 2, 4>); break;
+        case 2: few(linear_mx_rows_kernel<F, EX, 1, 8, 4, 4, 2>); break;
+        case 3: few(linear_mx_rows_kernel<F, EX, 1, 8, 8, 2, 2>); break;
+        case 4: few(linear_mx_rows_kernel<F, EX, 2, 8, 1, F == DARD_MX_FP8 ? 2 : 3, 4>); break;
+        case 5: few(linear_mx_rows_kernel<F, EX, 2, 16, 4, 2, 4>); break;
+        case 6: few(linear_mx_rows_kernel<F, EX, 4, 8, 1, 3, 2>); break;
         default: launch(linear_mx_tile_kernel<F, EX>, g, dim3(256), 0, s, a, tm, tn);
     }
 }

@@ -233,7 +233,7 @@ def test_linear_error_norm(fmt, M, N, K):
 # chunks of scales that are refilled, K that ends inside a unit
 CHOICES = [(1, 70, 1056), (1, 8230, 544), (1, 16520, 800), (33, 33010, 32), (33, 8230, 800), (1000, 12300, 32),
            (1, 16520, 32), (100, 33010, 32), (5, 33010, 6240), (5, 16520, 12320), (5, 8230, 33056), (64, 520, 33056),
-           (40, 33010, 6240), (40, 8230, 33056), (100, 33010, 6240), (600, 8230, 4128), (2050, 4130, 2080), (1030, 33010, 288)]
+           (40, 33010, 6240), (40, 8230, 33056), (100, 33010, 6240), (600, 8230, 4128), (2050, 4130, 2080), (1030, 33010, 288), (33, 16520, 12320), (1, 70, 3360)]
 
 
 @pytest.mark.parametrize("M,N,K", CHOICES)
