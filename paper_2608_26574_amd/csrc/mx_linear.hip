@@ -257,7 +257,7 @@ __device__ __forceinline__ void merge_rows(const LinArgs& a, const floatx16 (&ac
 // weights and their scales go from memory straight to registers, rows of x through LDS, shared
 // by the column waves of a group; both D units (256 k) deep.
 // With few rows bound by the weights: 32 x 126464 x 4096 takes 53 us, 5.2 TB/s of weights, one row x 4096 x
-// 4096 6.6 (latency: 16 units of a wave's serial loads).  With more, by the widening next to
+// 4096 6.6 (latency: a launch, two units a wave, the merge).  With more, by the widening next to
 // the matrix instructions: exact, 64 x 24576 x 4096 17.5 us (0.74 PFLOP/s on 192 CUs), 1024 x 3584 x
 // 18944 125 us (1.11 PFLOP/s); to bf16 14.5 and 70 us.
 template <int F, bool EX, int TI, int NW, int KG, int D, int OCC>
