@@ -523,8 +523,8 @@ dard_status dard_resid_norm_mx(float* h, int delta_dtype, const void* delta, int
  * [N][K/32]) out in the order the kernels read it (not a hot call); Wp holds
  * dard_packed_mx_bytes(N, K) bytes, 16-byte aligned.
  * dard_linear_mx: x [M][K] in `format`; Y [M][N] float32 or bf16 (out_dtype).
- * Needs M, N >= 1, K % 32 == 0, K <= 2^20, M * N < 2^39 and a W under 2^31 code
- * bytes; any N.
+ * Needs M, N >= 1, K % 32 == 0, K <= 2^20, M <= 2^30, M * N < 2^39 and a W under
+ * 2^31 code bytes; any N.
  * Workspace: dard_linear_mx_workspace_bytes(...) bytes, 16-byte aligned (0: none
  * is needed, ws may be NULL, which holds for every product of this version); its
  * contents need no initialisation. */

@@ -508,7 +508,7 @@ int check_mx_weight(int N, int K) {
 int check_mx_product(int M, int N, int K) {
     if (M < 1) return fail(DARD_ERR_SHAPE, "need M >= 1");
     if (int rc = check_mx_weight(N, K)) return rc;
-    if ((int64_t)M * N >= (int64_t)1 << 39) return fail(DARD_ERR_SHAPE, "need M * N < 2^39");
+    if (M > 1 << 30 || (int64_t)M * N >= (int64_t)1 << 39) return fail(DARD_ERR_SHAPE, "need M <= 2^30 and M * N < 2^39");
     return DARD_OK;
 }
 

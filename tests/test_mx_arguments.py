@@ -193,6 +193,7 @@ def test_size_limits():
     L = dard.lib()
     assert L.dard_packed_mx_bytes(1, (1 << 20) + 32) == 0 and L.dard_packed_mx_bytes(1, 1 << 20) > 0
     assert L.dard_linear_mx(0, P, P, 1 << 30, 32, P, 1 << 20, 0, P, None, 0, None) == -2
+    assert L.dard_linear_mx(0, P, P, 2 ** 31 - 1, 32, P, 1, 0, P, None, 0, None) == -2
     assert L.dard_resid_norm_mx(P, 0, None, 0, P, 1e-5, 1 << 24, 32, 0, P, P, None) == -2
     assert L.dard_quantize_mx(0, P, 32, 1 << 30, 32, 0, P, P, None) == -2
     f = lambda b, scale: L.dard_masked_attention_mx(   # noqa: E731
