@@ -45,6 +45,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFloor = -1e30f;   // running-max floor (log2 units): exp2 of anything below it is 0
 constexpr float kBig = 256.f;      // a lane's probability sum over a tile that moves the running max
 constexpr int kTileKeys = 32;
+constexpr uint32_t kFarScale = 253;   // least scale code whose values can be infinite in bf16: 4 * 2^126
 constexpr int kVisWords = 2 * kMaxBlock / 32 + 2;   // 32-bit words of a row's visibility, padded
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -275,6 +276,42 @@ __device__ __forceinline__ void add_values(const RawV& v, const uint32_t (&p)[JT
     }
 }
 
+// O^T += what key j of a tile adds through its V blocks of large scales (bit j of far[b], b the block of 32 dims), in the rows
+// that see it (bit j of seen).
+template <int DH, int JT>
+__device__ __forceinline__ void add_far(const char* slot, int j, const uint32_t (&far)[DH / 32], const uint32_t (&seen)[JT],
+                                        const uint32_t (&p)[JT][8], int lr, int eta, floatx16 (&o)[JT][DH / 32]) {
+    constexpr int NT = DH / 32;
+    const uint8_t* const vc = reinterpret_cast<const uint8_t*>(slot) + Slot<DH>::kV + (j >> 3) * (4 * DH) + 2 * (j & 7);
+    const uint8_t* const vs = reinterpret_cast<const uint8_t*>(slot) + Slot<DH>::kVs + (j >> 3) * (DH / 4) + (j & 7);
+    float w[JT];   // key j's probability: element 8 (j / 16) + j % 8 of the lanes of half j / 8 % 2
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) {
+        uint32_t pair = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pair = e == 4 * (j >> 4) + (j & 7) / 2 ? p[jt][e] : pair;
+        pair = (uint32_t)__shfl((int)pair, lr + 32 * ((j >> 3) & 1), 64);
+        w[jt] = __uint_as_float(j & 1 ? pair & 0xFFFF0000u : pair << 16);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int b = (e / 4) * NT / 4, row = 8 * (e / 4) + 4 * eta + e % 4;   // A row: dims NT row .. NT row + NT - 1
+        if (((far[b] >> j) & 1u) == 0) continue;
+        const float f = mx_scale_f(vs[8 * b]);
+        const uint32_t x = NT == 4 ? (uint32_t)*reinterpret_cast<const uint16_t*>(vc + 16 * row) : (uint32_t)vc[16 * (row / 2) + row % 2];
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
+            const uint32_t v = t ? fp4x2_to_bf16x2<1>(x, f) : fp4x2_to_bf16x2<0>(x, f);
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt) {
+                if (((seen[jt] >> j) & 1u) == 0) continue;
+                o[jt][t][e] = fmaf(w[jt], __uint_as_float(v << 16), o[jt][t][e]);
+                o[jt][t + 1][e] = fmaf(w[jt], __uint_as_float(v & 0xFFFF0000u), o[jt][t + 1][e]);
+            }
+        }
+    }
+}
+
 template <int DH, int JT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
@@ -455,38 +492,34 @@ void attn_mx_kernel(MxAttnArgs a, int rowtiles, int tps) {
             for (int e = 0; e < 16; ++e)
                 st[jt][e] = (bits >> (16 * (e / 8) + 8 * eta + e % 8)) & 1u ? st[jt][e] : -INFINITY;
         }
-        // a V block with a NaN scale would reach rows that do not see its key (0 * NaN):
-        // read it as zeros and note the key, per block of 32 dims
-        uint32_t mine = 0, bad[NT];
+        // A V block whose values may be infinite in bf16 (scale codes from kFarScale on) or are NaN would reach rows
+        // that do not see its key: 0 * infinity is NaN.  The matrix instructions read it with the least scale, and
+        // what it adds follows apart, row by row, for the keys of the sequence (bytes past them may be anything).
+        uint32_t far[NT], mine = 0;
 #pragma unroll
         for (int mm = 0; mm < 2; ++mm) {
             uint32_t sc[2] = {v.s[mm].x, v.s[mm].y};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (((sc[e / 4] >> (8 * (e & 3))) & 255u) == 255u) {
+                if (((sc[e / 4] >> (8 * (e & 3))) & 255u) >= kFarScale) {
                     mine |= 1u << (16 * mm + 8 * eta + e);
                     sc[e / 4] &= ~(255u << (8 * (e & 3)));
                 }
             }
             v.s[mm] = uintx2{sc[0], sc[1]};
         }
+        uint32_t keys = 0;   // those with such a block
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
             const int src = b * (32 / NT);
-            bad[b] = (uint32_t)__shfl((int)mine, src, 64) | (uint32_t)__shfl((int)mine, src + 32, 64);
+            far[b] = (uint32_t)__shfl((int)mine, src, 64) | (uint32_t)__shfl((int)mine, src + 32, 64);
+            keys |= far[b];
         }
         probabilities<JT, NT>(st, c, m, l, o, p);
         add_values<DH, JT>(v, p, lr, o);
-        if (__any(mine != 0)) {
-            // A row i of a block holds dim NT i + t, of the 32-dim block NT i / 32; element e has i / 8 = e / 4
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt)
-#pragma unroll
-                for (int t2 = 0; t2 < NT; ++t2)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (seen[jt] & bad[(e / 4) * NT / 4]) o[jt][t2][e] = __uint_as_float(0x7FC00000u);
-        }
+        keys = (uint32_t)__builtin_amdgcn_readfirstlane((int)keys) & (nkeys - k0 >= 32 ? ~0u : (1u << (nkeys - k0)) - 1u);
+#pragma unroll 1
+        for (; keys; keys &= keys - 1) add_far<DH, JT>(ring + at * Slot<DH>::kBytes, __builtin_ctz(keys), far, seen, p, lr, eta, o);
         refill(i);
     }
     __builtin_amdgcn_s_waitcnt(0);   // no copy lands after this point

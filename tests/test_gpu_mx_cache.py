@@ -90,6 +90,23 @@ def test_write_not_finite():
     assert nan_v[0, 8, 0, :32].all() and nan_v.sum() == 32
 
 
+def test_read_every_code_and_scale():
+    """Every E2M1 code with every scale out of the cache, in both types: exact, infinite from 2^128 on, NaN of 255."""
+    announce("kv read all")
+    Hkv, dh, n = 4, 64, 32
+    scales = np.arange(Hkv * n * 2, dtype=np.int64).reshape(1, Hkv, n, 2).astype(np.uint8)
+    codes = np.broadcast_to(np.arange(32) * 17 % 272, (1, Hkv, n, 32)).astype(np.uint8)
+    vc, vs = R.grouped(codes, scales[:, ::-1].copy())
+    cache = [dev(t) for t in (codes, scales, vc, vs)]
+    with np.errstate(over="ignore"):
+        want = [R.values(R.unpack(codes, R.FP4), s, R.FP4).astype(np.float32).transpose(0, 2, 1, 3) for s in (scales, scales[:, ::-1])]
+    for dtype in (torch.float32, torch.bfloat16):
+        k, v = (torch.empty(1, n, Hkv, dh, dtype=dtype, device="cuda") for _ in range(2))
+        dard.dard_kv_read_mx(cache, 0, k, v)
+        for got, ref in zip((k, v), want):
+            assert np.array_equal(got.float().cpu().numpy(), ref, equal_nan=True), dtype
+
+
 # ------------------------------------------------------------------ attention
 def block(b, B, seed, frac=(0.4, 0.3)):
     rng = np.random.default_rng(seed)
@@ -289,6 +306,90 @@ def test_attention_cache_past_4_gib():
         m = mn
     err = (out[s, :, h].double() - o / l[:, None]).abs()
     assert bool((err <= (2.0 ** -7 + 2.0 ** -12) * mass / l[:, None]).all())
+
+
+# ------------------------------------------------------------------ values past bf16's range, bytes never written
+def check_attention(q, cache, lens, P, state, conf, special=None):
+    """The attention of numpy cache arrays against float64.  Values of 2^128 and more are infinite, as bf16
+    has them; `special` is the one block position whose values may be (infinite results must then be of its sign,
+    and only in rows that see it)."""
+    b, R2, Hq, dh = q.shape
+    B, Hkv = R2 // 2, cache[0].shape[1]
+    out = torch.full_like(q, 3.0)
+    room = torch.full((dard.dard_attention_mx_workspace_bytes(b, B, Hq, Hkv, dh, P) // 4,), float("nan"), device="cuda")
+    prefix = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    dard.dard_masked_attention_mx(q, [dev(t) for t in cache], P, dev(state), dev(conf), dh ** -0.5, 0, out, ws=room, prefix=prefix)
+    got, qn = out.double().cpu().numpy(), q.double().cpu().numpy()
+    rc, rs = R.rows_of_cache(cache[2], cache[3])
+    for s in range(b):
+        p0 = P if lens is None else lens[s]
+        n = p0 + R2
+        seen = visible(state[s], conf[s], p0, 0)
+        for h in range(Hq):
+            kv = h // (Hq // Hkv)
+            k = R.values(R.unpack(cache[0][s, kv, :n], R.FP4), cache[1][s, kv, :n], R.FP4)
+            v = R.values(R.unpack(rc[s, kv, :n], R.FP4), rs[s, kv, :n], R.FP4)
+            far = np.abs(v) >= 2.0 ** 128
+            ref, bound = attend(qn[s, :, h], k, np.where(far, 0.0, v), seen, dh ** -0.5)
+            g = got[s, :, h]
+            if special is not None:
+                hit = seen[:, p0 + special, None] & far[p0 + special]
+                assert np.array_equal(g[hit], np.broadcast_to(np.copysign(np.inf, v[p0 + special]), g.shape)[hit]), (s, h)
+                g, ref, bound = g[~hit], ref[~hit], bound[~hit]
+            assert np.all(np.abs(g - ref) <= bound), (s, h, int(np.isnan(g).sum()))
+
+
+def filled_cache(b, Hkv, cap, dh, first, n, fill, seed):
+    """A cache with n written keys from 0 to first[s] + n; the other keys hold `fill` = (scale, code) bytes, or random ones."""
+    rng = np.random.default_rng(seed)
+    shapes = [t.shape for t in empty_cache(b, Hkv, cap, dh, 0)]
+    if fill is None:
+        start = [rng.integers(0, 256, sh, dtype=np.uint8) for sh in shapes]
+    else:
+        start = [np.full(sh, fill[0] if i % 2 else fill[1], np.uint8) for i, sh in enumerate(shapes)]
+    for s, p in enumerate(first):
+        part = [t[s:s + 1] for t in start]
+        k, v = rng.standard_normal((2, 1, p + n, Hkv, dh))
+        for t, w in zip(part, written(part, k, v, [0])):
+            t[...] = w
+    return start
+
+
+FILLS = [(0xFD, 0x77), (0xFE, 0x77), (0xFE, 0xC4), (0xFF, 0xFF), None]
+# rows of a KV head under and over 32, keys split over workgroups, prefixes of different lengths
+UNWRITTEN = [(2, 5, 27, 2, 2, 64, None), (1, 12, 45, 4, 2, 128, None), (1, 20, 6000, 2, 1, 64, None),
+             (3, 8, 100, 4, 4, 128, [0, 100, 33]), (2, 17, 90, 4, 2, 64, [3, 71])]
+
+
+@pytest.mark.parametrize("fill", FILLS)
+@pytest.mark.parametrize("b,B,P,Hq,Hkv,dh,lens", UNWRITTEN)
+def test_attention_unwritten_keys_hold_anything(fill, b, B, P, Hq, Hkv, dh, lens):
+    """Keys past those written, in the last tile and behind it, change nothing, whatever their bytes."""
+    announce("attention mx unwritten keys", fill, b, B, P, Hq, Hkv, dh, lens)
+    cap = -(-(P + 2 * B) // 32) * 32 + 32
+    cache = filled_cache(b, Hkv, cap, dh, [P] * b if lens is None else lens, 2 * B, fill, B)
+    state, conf = block(b, B, 11)
+    q = torch.from_numpy(np.random.default_rng(B).standard_normal((b, 2 * B, Hq, dh))).bfloat16().cuda()
+    check_attention(q, cache, lens, P, state, conf)
+
+
+@pytest.mark.parametrize("scale", [0xFC, 0xFD, 0xFE])
+@pytest.mark.parametrize("j", [0, 5, 12 + 5, 23])
+@pytest.mark.parametrize("Hq,Hkv,dh,P", [(4, 2, 128, 40), (2, 2, 64, 27), (2, 1, 64, 1)])
+def test_attention_values_past_bf16_reach_only_rows_that_see_them(scale, j, Hq, Hkv, dh, P):
+    """Block key j with a V block of the largest scales: infinite from 2^128 on, other values exact, and only
+    in the rows that see the key."""
+    announce("attention mx far values", scale, j, Hq, Hkv, dh, P)
+    B = 12
+    cache = filled_cache(1, Hkv, 96, dh, [P], 2 * B, (0xFF, 0xFF), 5)
+    rc, rs = (t.copy() for t in R.rows_of_cache(cache[2], cache[3]))
+    rs[0, Hkv - 1, P + j, dh // 32 - 1] = scale
+    rc[0, Hkv - 1, P + j, -16:] = np.arange(16) * 17   # every code
+    cache[2:] = R.grouped(rc, rs)
+    state, conf = block(1, B, 12)
+    # (scores near zero: no probability is under 2^-13, so none of the products underflows)
+    q = torch.from_numpy(np.random.default_rng(3).standard_normal((1, 2 * B, Hq, dh)) * 0.2).bfloat16().cuda()
+    check_attention(q, cache, None, P, state, conf, special=j)
 
 
 # ------------------------------------------------------------------ the operators together
