@@ -42,7 +42,7 @@ namespace dard {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kFloor = -1e30f;   // running-max floor (log2 units): exp2 of anything below it is 0
+constexpr float kFloor = -3.402823466e38f;   // start of a running maximum (log2 units): the least finite score
 constexpr float kBig = 256.f;      // a lane's probability sum over a tile that moves the running max
 constexpr int kTileKeys = 32;
 constexpr uint32_t kFarScale = 253;   // least scale code whose values can be infinite in bf16: 4 * 2^126

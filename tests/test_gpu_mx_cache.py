@@ -392,6 +392,25 @@ def test_attention_values_past_bf16_reach_only_rows_that_see_them(scale, j, Hq, 
     check_attention(q, cache, None, P, state, conf, special=j)
 
 
+@pytest.mark.parametrize("B,P,Hq,Hkv,dh", [(4, 70, 2, 1, 64), (20, 100, 2, 1, 128), (2, 9000, 2, 1, 64)])
+def test_attention_scores_far_below_zero(B, P, Hq, Hkv, dh):
+    """Every score of a row under -2^103: the largest of them still decides."""
+    announce("attention mx far scores", B, P, Hq, Hkv, dh)
+    cap = -(-(P + 2 * B) // 32) * 32
+    cache = filled_cache(1, Hkv, cap, dh, [P], 2 * B, (0xFF, 0xFF), 7)
+    cache[0][:], cache[1][:] = 0x22, 127 + 50          # every key 2^50
+    at = P - 9
+    cache[0][0, :, at] = 0x11                          # but one, half of it
+    state, conf = block(1, B, 13)
+    q = torch.full((1, 2 * B, Hq, dh), -2.0 ** 52, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 3.0)
+    room = torch.empty(dard.dard_attention_mx_workspace_bytes(1, B, Hq, Hkv, dh, P), dtype=torch.uint8, device="cuda")
+    dard.dard_masked_attention_mx(q, [dev(t) for t in cache], P, dev(state), dev(conf), dh ** -0.5, 0, out, ws=room)
+    rc, rs = R.rows_of_cache(cache[2], cache[3])
+    v = R.values(R.unpack(rc[0, 0, at], R.FP4), rs[0, 0, at], R.FP4)
+    assert np.array_equal(out.double().cpu().numpy(), np.broadcast_to(v, out.shape))
+
+
 # ------------------------------------------------------------------ the operators together
 def test_layer_half_captured_and_replayed():
     """Norm, QKV product, cache write, attention, quantised output, O product and the next norm, as a
