@@ -558,7 +558,7 @@ dard_status dard_linear_mx(int format, const void* codes, const uint8_t* scales,
  *   dard_masked_attention_mx   dard_masked_attention over this cache: q and out
  *     [b][2B][Hq][dh] bf16; sequence s has its prefix at keys 0 .. p - 1, p =
  *     prefix[s] or P, and its block (x, then s) at p .. p + 2B - 1.  Needs
- *     P + 2B <= cap and a finite scale > 0.  K and V are widened to bf16 (exact; 2^128 and more, which no written key
+ *     P + 2B <= cap and 0 < scale < 2^127.  K and V are widened to bf16 (exact; 2^128 and more, which no written key
  *     holds, is infinite), probabilities rounded to bf16, sums and statistics float32.  A NaN block or an infinite
  *     value reaches only the rows that see its key.  Workspace as for dard_linear_mx. */
 dard_status dard_kv_write_mx(int dtype, const void* k, const void* v, int64_t ld, int b, int n, int Hkv,

@@ -584,7 +584,8 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
                                      int b, int B, int Hq, int Hkv, int dh, float scale, uint32_t flags, void* out,
                                      void* ws, size_t ws_bytes, void* stream) {
     if (!q || !state || !conf || !out) return fail(DARD_ERR_ARG, "NULL pointer");
-    if (!(scale > 0.f && scale < INFINITY)) return fail(DARD_ERR_ARG, "need a finite scale > 0");
+    // (the kernel takes scale * log2(e) as a float)
+    if (!(scale > 0.f && scale < 0x1p127f)) return fail(DARD_ERR_ARG, "need 0 < scale < 2^127");
     if (int rc = check_flags(flags)) return rc;
     if (int rc = check_mx_attention(b, B, Hq, Hkv, dh, P)) return rc;
     if (int rc = check_mx_cache(kc, ks, vc, vs, b, Hkv, dh, cap)) return rc;

@@ -201,3 +201,12 @@ def test_size_limits():
     assert f(1 << 22, 0.1) == -2   # 2^24 workgroups
     for scale in (0.0, -0.1, float("inf"), float("nan")):
         assert f(1, scale) == -1
+
+
+def test_attention_scale_limit():
+    """scale * log2(e), which the kernel takes, has to be a float32 too."""
+    L = dard.lib()
+    f = lambda scale: L.dard_masked_attention_mx(   # noqa: E731
+        P, P, P, P, P, 10, None, 64, P, P, 1, 1, 4, 4, 128, scale, 0, P, None, 0, None)
+    for scale in (2.0 ** 127, 3.4e38):
+        assert f(scale) == -1 and b"scale" in L.dard_last_error()
