@@ -234,7 +234,7 @@ struct MxPacked {
 };
 inline MxPacked mx_packed(int N, int K) {
     MxPacked p;
-    p.nblk = (N + 31) / 32;
+    p.nblk = (N - 1) / 32 + 1;   // (N + 31 may pass 2^31)
     p.KBp = (K / 32 + 7) / 8 * 8;
     p.scales = (size_t)p.nblk * p.KBp * 512;
     p.total = p.scales + (size_t)p.nblk * p.KBp * 32;

@@ -210,3 +210,13 @@ def test_attention_scale_limit():
         P, P, P, P, P, 10, None, 64, P, P, 1, 1, 4, 4, 128, scale, 0, P, None, 0, None)
     for scale in (2.0 ** 127, 3.4e38):
         assert f(scale) == -1 and b"scale" in L.dard_last_error()
+
+
+def test_sizes_near_the_largest_int():
+    """Sizes that rounding up would take past 2^31 - 1 are refused, not wrapped."""
+    L = dard.lib()
+    top = 2 ** 31 - 1
+    for N in (top, top - 30):
+        L.dard_packed_mx_bytes(0, 0)
+        assert L.dard_packed_mx_bytes(N, 64) == 0 and b"2 GiB" in L.dard_last_error()
+    assert L.dard_packed_mx_bytes(64, top - 31) == 0 and b"2^20" in L.dard_last_error()
