@@ -506,7 +506,10 @@ dard_status dard_dequantize_mx(int format, const void* codes, const uint8_t* sca
  * does not depend on how the kernel splits a row.
  * h [rows][d] float32, updated in place; delta [rows][d] float32 or bf16
  * (delta_dtype) or NULL; gain [d] float32 or bf16 (gain_dtype).  Needs
- * d % 32 == 0, d <= 8192, rows < 2^24.  A row with an infinity or a NaN gives NaN blocks. */
+ * d % 32 == 0, d <= 8192, rows < 2^24.  As the formula has it, an infinity in a
+ * row (also one that the addition makes) gives a NaN block where it stands and
+ * zeros in the row's other blocks; a NaN, or a row of zeros with eps = 0, makes
+ * every block of the row NaN. */
 dard_status dard_resid_norm_mx(float* h, int delta_dtype, const void* delta, int gain_dtype,
                                const void* gain, float eps, int rows, int d, int format, void* codes,
                                uint8_t* scales, void* stream);

@@ -177,6 +177,31 @@ def test_resid_norm_not_finite():
     assert (s[2] == 255).all() and (s[1, 0] == 255) and (s[[0, 3]] != 255).all()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [96, 512, 4128])
+def test_resid_norm_rows_not_finite(fmt, d):
+    """An infinity (one that the addition makes, too) leaves NaN in its own block and zeros in the others of
+    its row, a NaN or, without eps, a row of zeros NaN everywhere; other rows keep their values."""
+    announce("resid norm rows not finite", fmt, d)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    h, dl = torch.randn(6, d, generator=g, device="cuda"), torch.randn(6, d, generator=g, device="cuda")
+    h[1, 40], h[2, d - 1] = float("inf"), float("nan")
+    h[3, 70] = dl[3, 70] = 3e38
+    h[4] = dl[4] = 0.0
+    gn = torch.ones(d, device="cuda")
+    with np.errstate(over="ignore"):
+        want_h, y = R.norm(h.cpu().numpy(), dl.cpu().numpy(), gn.cpu().numpy(), 0.0)
+    codes = torch.empty(code_shape(6, d, fmt), dtype=torch.uint8, device="cuda")
+    scales = torch.empty(6, d // 32, dtype=torch.uint8, device="cuda")
+    dard.dard_resid_norm_mx(h, gn, 0.0, fmt, codes, scales, delta=dl)
+    assert np.array_equal(h.cpu().numpy(), want_h, equal_nan=True)
+    s = scales.cpu().numpy()
+    nan = np.zeros_like(s, bool)
+    nan[1, 1] = nan[3, 2] = nan[2] = nan[4] = True
+    assert np.array_equal(s == 255, nan) and (s[[1, 3]][~nan[[1, 3]]] == 0).all()
+    check_codes(codes, scales, y, fmt)
+
+
 def mx_rows(rows, K, fmt, seed, spread=2.0):
     rng = np.random.default_rng(seed)
     x = rng.standard_normal((rows, K)) * np.exp2(rng.uniform(-spread, spread, (rows, K)))
