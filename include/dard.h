@@ -584,7 +584,9 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  * launches timed and their summed duration since the last reset.  Timing
  * events cost a few microseconds per launch; dard_trace_sample(n) times only
  * every n-th launch of each traced class (counted from the last reset;
- * 1 = every launch, the default). */
+ * 1 = every launch, the default).  dard_linear and dard_linear_mx count as
+ * DARD_K_GEMM_HEAD; packing, and the microscaled quantisation and cache calls,
+ * belong to no class. */
 #define DARD_K_GEMM_QKV   0
 #define DARD_K_GEMM_O     1
 #define DARD_K_GEMM_GU    2

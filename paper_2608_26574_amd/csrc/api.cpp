@@ -536,6 +536,7 @@ dard_status dard_linear_mx(int format, const void* codes, const uint8_t* scales,
     if (int rc = check_mx_product(M, N, K)) return rc;
     if (!aligned(codes, 16) || !aligned(Wp, 16)) return fail(DARD_ERR_ARG, "codes and Wp must be 16-byte aligned");
     if (!aligned(Y, esize(out_dtype))) return fail(DARD_ERR_ARG, "Y must be aligned to its element");
+    TraceScope ts(DARD_K_GEMM_HEAD, (hipStream_t)stream);   // (as dard_linear)
     HIPOK(launch_linear_mx(format, (const uint8_t*)codes, scales, M, K, Wp, N, out_dtype, Y, (hipStream_t)stream));
     return DARD_OK;
 }

@@ -503,3 +503,27 @@ def test_layer_half_captured_and_replayed():
     assert np.array_equal(h_.astype(np.float32), want)
     c, s8 = R.quantize(yn, R.FP8)
     assert np.array_equal(eager[1][4].cpu().numpy(), c) and np.array_equal(eager[1][5].cpu().numpy(), s8)
+
+
+def test_launches_are_traced():
+    """Norms, products and attention are timed by kernel class, as their other forms are."""
+    announce("mx trace")
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8, device="cuda")   # noqa: E731
+    codes, scales, wp = u8(3, 64), u8(3, 2), u8(dard.dard_packed_mx_bytes(64, 64))
+    cache = [dev(t) for t in empty_cache(1, 1, 32, 64, 0)]
+    q = torch.zeros(1, 2, 1, 64, dtype=torch.bfloat16, device="cuda")
+    y = torch.empty(3, 64, device="cuda")
+    dard.dard_trace_reset()
+    dard.dard_trace_enable((1 << dard.K_COUNT) - 1)
+    try:
+        dard.dard_resid_norm_mx(torch.ones(3, 64, device="cuda"), torch.ones(64, device="cuda"), 1e-5, dard.MX_FP8, codes, scales)
+        for _ in range(2):
+            dard.dard_linear_mx(dard.MX_FP8, codes, scales, wp, y)
+        dard.dard_masked_attention_mx(q, cache, 4, u8(1, 1), torch.zeros(1, 1, device="cuda"), 0.1, 0, torch.empty_like(q))
+    finally:
+        dard.dard_trace_enable(0)
+    counts = [dard.dard_trace_read(k) for k in range(dard.K_COUNT)]
+    dard.dard_trace_reset()
+    want = {dard.K_NORM: 1, dard.K_GEMM_HEAD: 2, dard.K_ATTENTION: 1}
+    assert [n for n, _ in counts] == [want.get(k, 0) for k in range(dard.K_COUNT)]
+    assert all(ms > 0 for n, ms in counts if n)
