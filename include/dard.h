@@ -539,6 +539,13 @@ dard_status dard_linear_mx(int format, const void* codes, const uint8_t* scales,
                            const void* Wp, int N, int out_dtype, void* Y, void* ws, size_t ws_bytes,
                            void* stream);
 
+/* What the library runs for such a product (a host-side query; nothing is
+ * launched): plan[0] x plan[1] = rows and columns of a workgroup, plan[2] =
+ * the groups of its waves among which K is split (0: the kernel that takes
+ * tiles through LDS, which splits no K), plan[3] = 1 where products are exact.
+ * plan: host int32 [4]. */
+dard_status dard_linear_mx_plan(int format, int M, int N, int K, int out_dtype, int32_t* plan);
+
 /* The MXFP4 key/value cache of one layer and the state-masked attention that
  * reads it: 17/32 of a byte per value, a quarter of a bf16 cache's 2 bytes and
  * half of FP8's.  Blocks of 32 lie along the head dim, so every key has scales

@@ -541,6 +541,14 @@ dard_status dard_linear_mx(int format, const void* codes, const uint8_t* scales,
     return DARD_OK;
 }
 
+dard_status dard_linear_mx_plan(int format, int M, int N, int K, int out_dtype, int32_t* plan) {
+    if (!plan) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (int rc = check_mx_types(format, out_dtype)) return rc;
+    if (int rc = check_mx_product(M, N, K)) return rc;
+    linear_mx_plan(format, out_dtype, M, N, K, plan);
+    return DARD_OK;
+}
+
 dard_status dard_kv_write_mx(int dtype, const void* k, const void* v, int64_t ld, int b, int n, int Hkv, int dh, int pos,
                              const int32_t* prefix, int cap, void* kc, uint8_t* ks, void* vc, uint8_t* vs, void* stream) {
     if (int rc = check_mx_kv(dtype, k, v, ld, kc, ks, vc, vs, b, n, Hkv, dh, pos, cap)) return rc;

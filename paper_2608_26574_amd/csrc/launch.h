@@ -250,6 +250,7 @@ hipError_t launch_pack_mx(const void* codes, const uint8_t* scales, int N, int K
 // Y = X W^T (float32 or bf16 [M][N]).
 hipError_t launch_linear_mx(int format, const uint8_t* xc, const uint8_t* xs, int M, int K, const void* Wp, int N,
                             int out_dtype, void* y, hipStream_t s);
+void linear_mx_plan(int format, int out_dtype, int M, int N, int K, int32_t* plan);
 // The MXFP4 cache of one layer: K codes [b][Hkv][cap][dh/2], scales
 // [b][Hkv][cap][dh/32]; V in groups of 8 keys, codes
 // [b][Hkv][cap/8][dh/4][8][2], scales [b][Hkv][cap/8][dh/32][8].

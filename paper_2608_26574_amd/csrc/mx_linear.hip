@@ -659,6 +659,8 @@ constexpr Kind kKinds[] = {
     {256, 256, 0, 256, {8.8f, 7.2f, 11.1f}, {5.58f, 3.34f, 2.16f}},   // the tiled kernel
 };
 
+int column_of(int format, bool exact) { return format == DARD_MX_FP4 ? 2 : exact ? 0 : 1; }
+
 int kind_of(int column, int M, int N, int K) {
     const double units = (K / 32 + 7) / 8;
     double best = 1e300;
@@ -679,7 +681,7 @@ int kind_of(int column, int M, int N, int K) {
 }
 
 template <int F, bool EX> void run(const LinArgs& a, hipStream_t s) {
-    const int kind = kind_of(F == DARD_MX_FP4 ? 2 : EX ? 0 : 1, a.M, a.N, a.K);
+    const int kind = kind_of(column_of(F, EX), a.M, a.N, a.K);
     const Kind& k = kKinds[kind];
     const int tm = (a.M + k.rows - 1) / k.rows, tn = (a.N + k.cols - 1) / k.cols;
     const dim3 g((unsigned)tm * tn);
@@ -702,6 +704,15 @@ template <int F, bool EX> void run(const LinArgs& a, hipStream_t s) {
 bool exact_of(int format, int out_dtype) { return format == DARD_MX_FP8 && out_dtype == DARD_DTYPE_F32; }
 
 }  // namespace
+
+void linear_mx_plan(int format, int out_dtype, int M, int N, int K, int32_t* plan) {
+    const bool exact = exact_of(format, out_dtype);
+    const Kind& k = kKinds[kind_of(column_of(format, exact), M, N, K)];
+    plan[0] = k.rows;
+    plan[1] = k.cols;
+    plan[2] = k.kg;
+    plan[3] = exact;
+}
 
 hipError_t launch_linear_mx(int format, const uint8_t* xc, const uint8_t* xs, int M, int K, const void* Wp, int N,
                             int out_dtype, void* y, hipStream_t s) {

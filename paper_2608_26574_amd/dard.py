@@ -38,7 +38,7 @@ EXPORTS = [
     "dard_workspace_bytes", "dard_prefill", "dard_prefill_extend", "dard_step", "dard_step_full", "dard_prefill_suffix",
     "dard_step_shared", "dard_pack_matrix", "dard_linear", "dard_gemm_plan",
     "dard_quantize_mx", "dard_dequantize_mx", "dard_resid_norm_mx", "dard_packed_mx_bytes", "dard_pack_matrix_mx",
-    "dard_linear_mx_workspace_bytes", "dard_linear_mx", "dard_kv_write_mx", "dard_kv_read_mx",
+    "dard_linear_mx_workspace_bytes", "dard_linear_mx", "dard_linear_mx_plan", "dard_kv_write_mx", "dard_kv_read_mx",
     "dard_attention_mx_workspace_bytes", "dard_masked_attention_mx",
     "dard_trace_enable",
     "dard_trace_read", "dard_trace_reset", "dard_trace_sample",
@@ -114,6 +114,7 @@ def lib():
             "dard_pack_matrix_mx": (i32, [vp, vp, i32, i32, vp, vp]),
             "dard_linear_mx_workspace_bytes": (sz, [i32, i32, i32, i32]),
             "dard_linear_mx": (i32, [i32, vp, vp, i32, i32, vp, i32, i32, vp, vp, sz, vp]),
+            "dard_linear_mx_plan": (i32, [i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_int32)]),
             "dard_kv_write_mx": (i32, [i32, vp, vp, i64, i32, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]),
             "dard_kv_read_mx": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, i64, vp]),
             "dard_attention_mx_workspace_bytes": (sz, [i32, i32, i32, i32, i32, i32]),
@@ -381,6 +382,16 @@ def dard_pack_matrix_mx(codes, scales, Wp, stream=None):
 
 def dard_linear_mx_workspace_bytes(format, M, N, K):
     return lib().dard_linear_mx_workspace_bytes(format, M, N, K)
+
+
+def dard_linear_mx_plan(format, M, N, K, out=torch.float32):
+    """(workgroup rows, workgroup columns, parts of K in a workgroup or 0, exact products) that the library runs
+    for a product with results of type `out`."""
+    if out is not torch.float32 and out is not torch.bfloat16:
+        raise ValueError(f"out must be bfloat16 or float32, got {out}")
+    plan = (ctypes.c_int32 * 4)()
+    _check(lib().dard_linear_mx_plan(format, M, N, K, DTYPE_BF16 if out is torch.bfloat16 else DTYPE_F32, plan))
+    return tuple(plan)
 
 
 def dard_linear_mx(format, codes, scales, Wp, Y, ws=None, stream=None):
