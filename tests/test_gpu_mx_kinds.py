@@ -112,6 +112,52 @@ def test_exact_sums(kind, fmt, out, M, N, K):
 
 @gpu
 @pytest.mark.parametrize("kind,M,N,K", EXACT)
+def test_float32_products_are_exact(kind, M, N, K):
+    """Eight neighbouring products that span 2^16, two large ones that cancel among them: the small ones count.
+    All sums are multiples of u = 2^-8 below 2^24 u in any order (float32 holds them): at most 200 of a
+    row's groups have a pair of +-2^8 = 2^16 u, the other products are 12 u at most."""
+    announce("linear kinds, exact products", kind, M, N, K)
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    w = torch.tensor([1, 2, 9, 10], dtype=torch.uint8, device="cuda")[ints(g, 0, 4, N, K // 2).long()].repeat_interleave(2, 1)
+    ws = (127 - torch.arange(N, device="cuda") % 2).to(torch.uint8)[:, None].repeat(1, K // 32)          # (a factor of
+    xs = (127 + torch.arange(M, device="cuda") % 3).to(torch.uint8)[:, None].repeat(1, K // 32)          # the result)
+    small = torch.tensor([0x08, 0x0C, 0x10, 0x14, 0x88, 0x8C, 0x90, 0x94], dtype=torch.uint8, device="cuda")   # 1 to 3 times 2^-6
+    x = small[ints(g, 0, 8, M, K).long()].view(M, K // 8, 4, 2)
+    large = torch.rand(M, K // 8, generator=g, device="cuda") < min(0.5, 80 / (K // 8))
+    assert int(large.sum(1).max()) <= 200 and 200 * 2 ** 16 + 12 * K < 2 ** 24
+    pair = torch.randint(0, 4, (M, K // 8), generator=g, device="cuda")
+    at = large[:, :, None] & (pair[:, :, None] == torch.arange(4, device="cuda"))
+    x[at] = torch.tensor([0x78, 0xF8], dtype=torch.uint8, device="cuda")                                 # 256, -256
+    x = x.view(M, K)
+    wv = values(w, ws, dard.MX_FP4)
+    ref = (values(x, xs, dard.MX_FP8) @ wv.T).float()
+    got = product(dard.MX_FP8, x, xs, packed(w, ws), N, F32)
+    assert torch.equal(got, ref), float((got != ref).float().mean())
+    # the test can tell: cut 13 bits below the largest, the small products of those groups would be gone
+    cut = torch.where(large[:, :, None].expand(-1, -1, 8).reshape(M, K) & ~at.repeat_interleave(2, 2).view(M, K), x, 0)
+    assert float(((values(cut, xs, dard.MX_FP8) @ wv.T) != 0).float().mean()) > 0.9
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(48, 512, 4096), (320, 256, 3584)])
+def test_float32_error_norm(M, N, K):
+    """K / 16 rounded additions, each within 2^-24 of a partial sum: at random, 2^-24 sqrt(K / 32) = 7e-7 of the
+    result at most at these K (products cut 13 bits below the largest of eight leave 4.5e-6)."""
+    announce("linear kinds, error norm", M, N, K)
+    g = torch.Generator(device="cuda").manual_seed(K)
+    x, w = torch.randn(M, K, generator=g, device="cuda"), torch.randn(N, K, generator=g, device="cuda")
+    xc, xs = torch.empty(M, K, dtype=torch.uint8, device="cuda"), torch.empty(M, K // 32, dtype=torch.uint8, device="cuda")
+    wc, ws = torch.empty(N, K // 2, dtype=torch.uint8, device="cuda"), torch.empty(N, K // 32, dtype=torch.uint8, device="cuda")
+    dard.dard_quantize_mx(x, dard.MX_FP8, xc, xs)
+    dard.dard_quantize_mx(w, dard.MX_FP4, wc, ws)
+    codes = torch.stack([wc & 15, wc >> 4], -1).flatten(1)
+    ref = values(xc, xs, dard.MX_FP8) @ values(codes, ws, dard.MX_FP4).T
+    got = product(dard.MX_FP8, xc, xs, packed(codes, ws), N, F32).double()
+    assert float((got - ref).norm() / ref.norm()) <= 2.0 ** -24 * (K / 32) ** 0.5
+
+
+@gpu
+@pytest.mark.parametrize("kind,M,N,K", EXACT)
 def test_high_scales_stay_local(kind, M, N, K):
     """Scale codes past those of quantised float32 in one row of x and one of w: their results are right, the
     others keep their bits."""
