@@ -198,9 +198,10 @@ __device__ __forceinline__ KvItem kv_item(const MxKvArgs& a, uint32_t i) {
     return {(int)(i & ((1u << sh) - 1)), (int)(key - st * a.Hkv), (int)(st - s * a.n), (int)s};
 }
 
-// One thread per 8 dims of one key of K (blockIdx.y = 0) or V (1).  8192 float32 keys of 4 heads x 128
-// take 9.6 us (38 MB: V's two bytes a thread go out in 16-byte runs of 8 keys), reading them back as
-// bf16 7.4 us (21 MB); 64 keys of 32 heads 3.1 us each.
+// One thread per 8 dims of one key of K (blockIdx.y = 0) or V (1), a key's dims and heads next to each other.  Bound
+// by bytes and, for V, by accesses: a lane's codes are two bytes here and two 16 bytes on, the other keys of the group
+// lie between.  8192 float32 keys of 4 heads x 128 take 9.1 us (38 MB), reading them back as bf16 7.2 us
+// (21 MB); 64 keys of 32 heads 3.0 us each.
 template <typename T>
 __global__ __launch_bounds__(256) void kv_write_mx_kernel(MxKvArgs a, const T* __restrict__ k, const T* __restrict__ v) {
     const KvItem item = kv_item(a, blockIdx.x * 256u + threadIdx.x);
