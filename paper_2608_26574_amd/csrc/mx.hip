@@ -35,8 +35,8 @@ template <int F> __device__ __forceinline__ uint2 quantize8(const float (&v)[8],
     return mx_encode8<F>(t);
 }
 
-// At the rate of a copy: 8192 x 3584 bf16 from memory to MXFP4 in 16.6 us, 4.5 TB/s (to MXFP8 19.5 us, float32 to
-// MXFP4 24.3, 5.5 TB/s); four chunks a thread in flight gain nothing.  Right behind a product that left its
+// At the rate of a copy: 8192 x 3584 bf16 from memory to MXFP4 in 16.1 us, 4.6 TB/s (to MXFP8 19.5 us, float32 to
+// MXFP4 23.7, 5.6 TB/s); four chunks a thread in flight gain nothing.  Right behind a product that left its
 // output dirty in the caches the same call takes 24 us.
 template <typename T, int F>
 __global__ __launch_bounds__(256) void quantize_mx_kernel(const T* __restrict__ x, int64_t ld, uint32_t nchunk, uint32_t cpr,
@@ -53,6 +53,8 @@ __global__ __launch_bounds__(256) void quantize_mx_kernel(const T* __restrict__ 
     if ((c & 3) == 0) scales[c >> 2] = (uint8_t)scale;
 }
 
+// Bound by its bytes: 8192 x 3584 MXFP8 to bf16 in 18.5 us, 4.8 TB/s (MXFP4 18.7, 4.0 TB/s), to float32 29.8 us, 5.0
+// TB/s (MXFP4 29.9, 4.4).
 template <typename T, int F>
 __global__ __launch_bounds__(256) void dequantize_mx_kernel(const uint8_t* __restrict__ codes,
                                                             const uint8_t* __restrict__ scales, uint32_t nchunk,
@@ -76,7 +78,7 @@ __global__ __launch_bounds__(256) void dequantize_mx_kernel(const uint8_t* __res
 // in 64 bits up to the element's rounding (the memory traffic hides it): an
 // 8-bit step is so coarse that a last bit of a float32 sum, which depends on
 // how a row is split, would now and then move a value by a whole step.
-// Bound by its bytes: 8192 x 3584 with a bf16 delta to MXFP8 in 64.1 us, 5.06 TB/s, a
+// Bound by its bytes: 8192 x 3584 with a bf16 delta to MXFP8 in 63.9 us, 5.07 TB/s, a
 // copy's rate; 64 x 4096 in 4.6 us, a launch and two trips to memory.
 template <int NV, typename D, typename G, int F>
 __global__ __launch_bounds__(256) void resid_norm_mx_kernel(float* __restrict__ h, const D* __restrict__ delta,

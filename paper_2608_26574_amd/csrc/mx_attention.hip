@@ -12,12 +12,12 @@
 // merged in split order by a second kernel).
 //
 // What bounds it: per tile and 64 rows 32 matrix instructions and about 250
-// others, of which 64 widen codes, 32 pair V's keys and 32 are exp2.  On random
-// data the matrix instructions alone run at 1.55 PFLOP/s (clocks fall under their
-// power) and a mix in these proportions, two waves a SIMD, takes 0.89 us a tile and
-// SIMD; the main loop takes 1.04.  Two waves a SIMD with the queries in LDS (read
-// anew for every tile) beat one wave with them in registers, 133 to 170 us at 448 rows
-// and 131136 keys, though that one alternates both kinds of instruction by hand.
+// others, of which 64 widen codes, 32 pair V's keys and 32 are exp2.  Counters at 448 rows and
+// 131136 keys (131 us): vector instructions issue in 75% of a SIMD's cycles, the matrix
+// unit is busy in 64%; a tile takes a SIMD 0.84 us (the difference of 98368 and 131136 keys).  Two
+// waves a SIMD with the queries in LDS (read anew for every tile) beat one wave with them
+// in registers, 133 to 170 us at that size before the order of the waves below was set, though that
+// one alternates both kinds of instruction by hand.
 //
 // Operand order.  Lane l is row l % 32 of an operand, eta = l / 32.
 //   S^T: A row i holds key pi(i), pi swapping bits 2 and 3, and a lane's dims are
@@ -198,6 +198,10 @@ __device__ __forceinline__ void scores(const RawK<DH>& k, const bf16x8* q, int l
 // exceeds kBig (always on a row's first visible tile, and whenever a score is
 // more than 8 above m) has the tile's maximum taken, the accumulators rescaled
 // and the probabilities formed again, so other tiles need no maximum.
+// They are rounded to bf16, the type in which the matrix instruction takes
+// them (as in the framework's bf16 attention), and the row sum, in float32, is that of the rounded ones, so that the
+// weights add up to 1.  On ordinary data the result is then off by 0.0021 to 0.0023 of its norm, where the
+// bf16 output alone leaves 0.0017.
 template <int JT, int NT>
 __device__ __forceinline__ void probabilities(const floatx16 (&st)[JT], float c, float (&m)[JT], float (&l)[JT],
                                               floatx16 (&o)[JT][NT], uint32_t (&p)[JT][8]) {

@@ -256,10 +256,11 @@ __device__ __forceinline__ void merge_rows(const LinArgs& a, const floatx16 (&ac
 // narrow matrix keeps enough loads in flight without partial results in memory).  A wave's
 // weights and their scales go from memory straight to registers, rows of x through LDS, shared
 // by the column waves of a group; both D units (256 k) deep.
-// With few rows bound by the weights: 32 x 126464 x 4096 takes 53 us, 5.2 TB/s of weights, one row x 4096 x
-// 4096 6.6 (latency: a launch, two units a wave, the merge).  With more, by the widening next to
-// the matrix instructions: exact, 64 x 24576 x 4096 17.5 us (0.74 PFLOP/s on 192 CUs), 1024 x 3584 x
-// 18944 125 us (1.11 PFLOP/s); to bf16 14.5 and 70 us.
+// With few rows bound by the weights: 32 x 126464 x 4096 takes 56 us, 4.9 TB/s of weights, one row x 4096 x
+// 4096 6.7 (latency: a launch, two units a wave, the merge).  With more, by the widening next to
+// the matrix instructions: exact, 64 x 24576 x 4096 19.5 us (0.66 PFLOP/s on 192 CUs; counters: vector
+// instructions issue in 63% of a SIMD's cycles, the matrix unit is busy in 44%, a wave waits in 41% of its own), 1024 x
+// 3584 x 18944 131 us (1.06 PFLOP/s); to bf16 14 and 71 us.
 template <int F, bool EX, int TI, int NW, int KG, int D, int OCC>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void linear_mx_rows_kernel(LinArgs a, int tiles_m) {
@@ -440,8 +441,8 @@ void linear_mx_rows_kernel(LinArgs a, int tiles_m) {
 // The fragments of each step are read during the step before; the barrier of a stage
 // stands before its last step, where every wave holds the rest of the stage in registers. It
 // publishes the next stage and frees this one for a copy.
-// 8192 x 37888 x 3584 MXFP4 785 us, 2.83 PFLOP/s; 8192 x 8192 x 8192 MXFP4 354 us, 3.10, MXFP8 to bf16 473 us,
-// 2.32, exact 820 us, 1.34 (the bf16 instruction's rate on random data is 1.55).
+// 8192 x 37888 x 3584 MXFP4 786 us, 2.83 PFLOP/s; 8192 x 8192 x 8192 MXFP4 367 us, 2.99, MXFP8 to bf16 446 us,
+// 2.47, exact 776 us, 1.42 (the bf16 instruction's rate on random data is 1.55).
 template <int F, bool EX>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void linear_mx_tile_kernel(LinArgs a, int tiles_m, int tiles_n) {
@@ -643,7 +644,8 @@ void linear_mx_tile_kernel(LinArgs a, int tiles_m, int tiles_n) {
 // A kernel with its tile, and what it costs (us): a round of 256 workgroups takes fixed + unit per 256 k of
 // a workgroup's K range.  Fitted to a sweep of all kernels (and four that hardly pay: 32 x 128 and 64 x 64 in
 // eight waves, 32 x 192 in twelve, 64 x 256 in sixteen) over M 1 to 4096, N 3584 to 126464 and K 512 to 18944; the
-// choice by cost loses 2% to the best of all twelve for each size.  Columns: exact, MXFP8, MXFP4.
+// choice by cost loses 2% to the best of all twelve for each size there (smaller matrices take the same
+// formula and were not swept).  Columns: exact, MXFP8, MXFP4.
 struct Kind {
     int rows, cols, kg, threads;
     float fixed[3], unit[3];
