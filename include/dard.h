@@ -570,7 +570,8 @@ dard_status dard_linear_mx_plan(int format, int M, int N, int K, int out_dtype, 
  *     prefix[s] or P, and its block (x, then s) at p .. p + 2B - 1.  Needs
  *     P + 2B <= cap and 0 < scale < 2^127.  K and V are widened to bf16 (exact; 2^128 and more, which no written key
  *     holds, is infinite), probabilities rounded to bf16, sums and statistics float32.  A NaN block or an infinite
- *     value reaches only the rows that see its key.  Workspace as for dard_linear_mx. */
+ *     value reaches only the rows that see its key.  Workspace as for dard_linear_mx;
+ *     a longer prefix can need less of it, so a buffer for several P is sized for the largest need. */
 dard_status dard_kv_write_mx(int dtype, const void* k, const void* v, int64_t ld, int b, int n, int Hkv,
                              int dh, int pos, const int32_t* prefix, int cap, void* kc, uint8_t* ks,
                              void* vc, uint8_t* vs, void* stream);
