@@ -585,6 +585,75 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
                                      int dh, float scale, uint32_t flags, void* out, void* ws,
                                      size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------ shared prefixes and cache eviction
+ * Attention for a batch whose sequences share a prefix, the weight that every
+ * cached key got from it, and the cache cut to the keys that got most: the
+ * operators of a layer for long prompts (prefix caching, App. C.5) that a whole
+ * batch reads or that have outgrown their memory.  dtype is DARD_DTYPE_F32, _BF16
+ * or _BF16_KV_FP8, caches are those of dard_masked_attention (K [..][cap][dh], V
+ * dims-major [..][dh][cap]); q, out, K and V of the 16- and 8-bit types are 16-byte
+ * aligned, everything else as its element.  Sequences may have prefixes of
+ * different lengths: `prefix`, when not NULL, is a device array of b lengths,
+ * clamped into [0, P]; NULL: P each.
+ *
+ *   dard_masked_attention_shared  dard_masked_attention with a prefix of Ps shared
+ *     keys and then the sequence's own p = prefix[s] or P:
+ *       k_shared [Hkv][cap_shared][dh], v_shared [Hkv][dh][cap_shared]: keys
+ *         0 .. Ps - 1 of every sequence, read once for the whole batch
+ *         (any Ps >= 0; with 0 both may be NULL);
+ *       k [b][Hkv][cap][dh], v [b][Hkv][dh][cap]: own prefix at keys 0 .. p - 1,
+ *         the block (x, then s) at p .. p + 2B - 1.
+ *     lse [b][2B][Hq] float32, or NULL: the natural log of the row's sum of
+ *     e^(scale q . k) over the keys that it sees.  Needs Ps <= cap_shared, P + 2B <=
+ *     cap, P and Ps at most 2^30, 0 < scale < 2^127.  Probabilities are rounded to
+ *     bf16 (bf16, FP8 caches), sums and statistics are float32.  What stands in
+ *     keys that a row does not see, also infinities and NaN, does not reach it; a
+ *     row whose scores are all minus infinity gives zeros and lse = minus infinity.
+ *
+ *   dard_key_weights  for every prefix key j < p of every KV head g
+ *       weights[s][g][j] = decay weights[s][g][j] +
+ *                          sum over r < R, heads h of g of e^(scale q[s][r][h] . k_j - lse[s][r][h])
+ *     q [b][R][Hq][dh], lse [b][R][Hq] float32 (as the attention gave it; a row
+ *     whose lse is infinite counts nothing), k [b][Hkv][cap][dh]; weights
+ *     [b][Hkv] rows of float32, ldw >= P elements apart.  Sums of other keys keep
+ *     their values; decay = 0 does not read the old ones.  0 <= decay <= 1.  The
+ *     keys of a shared prefix, summed over a batch: b = 1, R = batch * 2B rows.
+ *     The order of the additions is fixed by the sizes.
+ *
+ *   dard_kv_select  the m = min(n, p) keys of every (s, g) that rank highest:
+ *     the first `first` and last `last` of the p keys always, then by weight,
+ *     the larger first, ties to the lower index (NaN ranks below everything, -0
+ *     as 0).  keep [b][Hkv][n] int32: their indices, ascending, then -1 from m
+ *     on; kept [b] int32 or NULL: m.  Needs n >= 1, first + last <= n.
+ *
+ *   dard_kv_compact  key j of every (s, g) becomes key keep[s][g][j], j < m =
+ *     kept[s] (NULL: n; at most n and p), in K, V and, when not NULL, weights, in
+ *     place; weights m .. p - 1 become 0, so that keys written there start from
+ *     nothing; every other key keeps its bytes.  keep ascends, as dard_kv_select
+ *     writes it (indices are clamped into [0, p); other orders give unspecified
+ *     keys).  With kept as the prefix of the next call, the block or new keys
+ *     follow at m.
+ *
+ * Workspaces (device, caller-owned, 16-byte aligned, contents need no
+ * initialisation) by the queries; 0: none is needed, ws may be NULL. */
+size_t dard_attention_shared_workspace_bytes(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P);
+dard_status dard_masked_attention_shared(int dtype, const void* q, const void* k_shared, const void* v_shared,
+                                         int Ps, int cap_shared, const void* k, const void* v, int P,
+                                         const int32_t* prefix, int cap, const uint8_t* state, const float* conf,
+                                         int b, int B, int Hq, int Hkv, int dh, float scale, uint32_t flags,
+                                         void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t dard_key_weights_workspace_bytes(int dtype, int b, int R, int Hq, int Hkv, int dh, int P);
+dard_status dard_key_weights(int dtype, const void* q, const float* lse, const void* k, int P,
+                             const int32_t* prefix, int cap, int b, int R, int Hq, int Hkv, int dh, float scale,
+                             float decay, float* weights, int64_t ldw, void* ws, size_t ws_bytes, void* stream);
+size_t dard_kv_select_workspace_bytes(int b, int Hkv, int P, int n);
+dard_status dard_kv_select(const float* weights, int64_t ldw, int P, const int32_t* prefix, int b, int Hkv,
+                           int n, int first, int last, int32_t* keep, int32_t* kept, void* ws, size_t ws_bytes,
+                           void* stream);
+dard_status dard_kv_compact(int dtype, void* k, void* v, int cap, float* weights, int64_t ldw,
+                            const int32_t* keep, int n, const int32_t* kept, int P, const int32_t* prefix,
+                            int b, int Hkv, int dh, void* stream);
+
 /* ------------------------------------------------------------ tracing
  * When enabled, the library brackets each launch of the kernel classes in
  * `class_mask` with HIP events on the launch stream.  dard_trace_read()
@@ -593,8 +662,8 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  * events cost a few microseconds per launch; dard_trace_sample(n) times only
  * every n-th launch of each traced class (counted from the last reset;
  * 1 = every launch, the default).  dard_linear and dard_linear_mx count as
- * DARD_K_GEMM_HEAD; packing, and the microscaled quantisation and cache calls,
- * belong to no class. */
+ * DARD_K_GEMM_HEAD; packing, the microscaled quantisation and cache calls, and
+ * key weights, selection and compaction belong to no class. */
 #define DARD_K_GEMM_QKV   0
 #define DARD_K_GEMM_O     1
 #define DARD_K_GEMM_GU    2

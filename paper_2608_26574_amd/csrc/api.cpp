@@ -614,6 +614,174 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
     return DARD_OK;
 }
 
+// ---------------------------------------------------------------- shared prefixes and eviction
+namespace {
+
+int check_kv_type(int dtype) {
+    if (dtype != DARD_DTYPE_F32 && dtype != DARD_DTYPE_BF16 && dtype != DARD_DTYPE_BF16_KV_FP8)
+        return fail(DARD_ERR_ARG, "unknown dtype %d", dtype);
+    return DARD_OK;
+}
+
+// 16-byte accesses of bf16 and FP8 tensors; fp32 ones are taken at any element
+uintptr_t kv_align(int dtype) { return dtype == DARD_DTYPE_F32 ? 4 : 16; }
+
+// scale * log2(e) is taken as a float
+int check_scale(float scale) {
+    return scale > 0.f && scale < 0x1p127f ? DARD_OK : fail(DARD_ERR_ARG, "need 0 < scale < 2^127");
+}
+
+int check_heads(int b, int Hq, int Hkv, int dh) {
+    if (b < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv) return fail(DARD_ERR_SHAPE, "need b, Hq, Hkv >= 1 and Hq %% Hkv == 0");
+    if (dh != 64 && dh != 128) return fail(DARD_ERR_SHAPE, "dh must be 64 or 128");
+    return DARD_OK;
+}
+
+int check_shared_attention(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P) {
+    if (int rc = check_kv_type(dtype)) return rc;
+    if (int rc = check_heads(b, Hq, Hkv, dh)) return rc;
+    if (B < 1 || B > 256 || Ps < 0 || P < 0) return fail(DARD_ERR_SHAPE, "need 1 <= B <= 256, Ps >= 0, P >= 0");
+    // (a workgroup counts the tiles of up to 64 sequences in an int)
+    if (Ps > (1 << 30) || P > (1 << 30)) return fail(DARD_ERR_SHAPE, "Ps and P must be at most 2^30");
+    if ((double)b * 2 * B * Hq * (dh / 4) > 2147483647.0) return fail(DARD_ERR_SHAPE, "too many query rows in one call");
+    return DARD_OK;
+}
+
+// Workspace of dard_masked_attention_shared: the state mask (bf16), then the partial results of a key split.
+struct SharedWs {
+    size_t part, total;
+};
+
+SharedWs shared_ws(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P) {
+    SharedWs w{};
+    w.part = dtype == DARD_DTYPE_F32 ? 0 : align256((size_t)b * 2 * B * ((B + 63) / 64) * 8);
+    w.total = w.part + shared_attention_partial_floats(dtype, b, B, Hq, Hkv, dh, Ps, P) * 4;
+    return w;
+}
+
+int check_key_weights(int dtype, int b, int R, int Hq, int Hkv, int dh, int P) {
+    if (int rc = check_kv_type(dtype)) return rc;
+    if (int rc = check_heads(b, Hq, Hkv, dh)) return rc;
+    if (R < 1 || P < 0) return fail(DARD_ERR_SHAPE, "need R >= 1 and P >= 0");
+    if ((double)R * Hq > 1073741824.0) return fail(DARD_ERR_SHAPE, "R * Hq must be at most 2^30");
+    if ((double)b * Hkv * (P / 128 + 1.0) >= 8388608.0) return fail(DARD_ERR_SHAPE, "too many keys in one call");
+    return DARD_OK;
+}
+
+}  // namespace
+
+size_t dard_attention_shared_workspace_bytes(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P) {
+    return check_shared_attention(dtype, b, B, Hq, Hkv, dh, Ps, P) ? 0 : shared_ws(dtype, b, B, Hq, Hkv, dh, Ps, P).total;
+}
+
+dard_status dard_masked_attention_shared(int dtype, const void* q, const void* k_shared, const void* v_shared, int Ps,
+                                         int cap_shared, const void* k, const void* v, int P, const int32_t* prefix,
+                                         int cap, const uint8_t* state, const float* conf, int b, int B, int Hq, int Hkv,
+                                         int dh, float scale, uint32_t flags, void* out, float* lse, void* ws,
+                                         size_t ws_bytes, void* stream) {
+    if (!q || !k || !v || !state || !conf || !out) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (Ps > 0 && (!k_shared || !v_shared)) return fail(DARD_ERR_ARG, "Ps > 0 needs the shared cache");
+    if (int rc = check_scale(scale)) return rc;
+    if (int rc = check_flags(flags)) return rc;
+    if (int rc = check_shared_attention(dtype, b, B, Hq, Hkv, dh, Ps, P)) return rc;
+    if (Ps > 0 && Ps > cap_shared) return fail(DARD_ERR_SHAPE, "Ps must be <= cap_shared");
+    if (2 * B > cap || P > cap - 2 * B) return fail(DARD_ERR_SHAPE, "P + 2B must be <= cap");
+    const uintptr_t al = kv_align(dtype);
+    if (!aligned(q, al) || !aligned(out, al) || !aligned(k, al) || !aligned(v, al) ||
+        (Ps > 0 && (!aligned(k_shared, al) || !aligned(v_shared, al))))
+        return fail(DARD_ERR_ARG, "q, out and the caches must be %d-byte aligned", (int)al);
+    if (!aligned(conf, 4) || !aligned(lse, 4) || !aligned(prefix, 4)) return fail(DARD_ERR_ARG, "conf, lse and prefix must be 4-byte aligned");
+    const SharedWs w = shared_ws(dtype, b, B, Hq, Hkv, dh, Ps, P);
+    if (w.total && (!ws || ws_bytes < w.total)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", w.total);
+    if (w.total && !aligned(ws, 16)) return fail(DARD_ERR_ARG, "the workspace must be 16-byte aligned");
+    SharedAttnArgs a{};
+    a.q = q; a.out = out; a.lse = lse;
+    a.ksh = k_shared; a.vsh = v_shared; a.k = k; a.v = v;
+    a.state = state; a.conf = conf; a.prefix = prefix;
+    a.Ps = Ps; a.cap_sh = cap_shared; a.P = P; a.cap = cap;
+    a.b = b; a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.dh = dh;
+    a.scale = scale; a.flags = flags;
+    a.part = (float*)((char*)ws + w.part);
+    hipStream_t s = (hipStream_t)stream;
+    TraceScope ts(DARD_K_ATTENTION, s);
+    if (dtype != DARD_DTYPE_F32) {
+        a.sel = (const uint64_t*)ws;
+        TraceScope tm(DARD_K_MASK, s);
+        HIPOK(launch_build_state_mask(state, conf, b, B, flags, (uint64_t*)ws, s));
+    }
+    HIPOK(launch_shared_attention(dtype, a, s));
+    return DARD_OK;
+}
+
+size_t dard_key_weights_workspace_bytes(int dtype, int b, int R, int Hq, int Hkv, int dh, int P) {
+    if (check_key_weights(dtype, b, R, Hq, Hkv, dh, P) || P == 0) return 0;
+    return key_weights_partial_floats(dtype, b, R, Hq, Hkv, P) * 4;
+}
+
+dard_status dard_key_weights(int dtype, const void* q, const float* lse, const void* k, int P, const int32_t* prefix,
+                             int cap, int b, int R, int Hq, int Hkv, int dh, float scale, float decay, float* weights,
+                             int64_t ldw, void* ws, size_t ws_bytes, void* stream) {
+    if (!q || !lse || !k || !weights) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (int rc = check_scale(scale)) return rc;
+    if (!(decay >= 0.f && decay <= 1.f)) return fail(DARD_ERR_ARG, "need 0 <= decay <= 1");
+    if (int rc = check_key_weights(dtype, b, R, Hq, Hkv, dh, P)) return rc;
+    if (P > cap || ldw < P) return fail(DARD_ERR_SHAPE, "P must be <= cap and <= ldw");
+    const uintptr_t al = kv_align(dtype);
+    if (!aligned(q, al) || !aligned(k, al)) return fail(DARD_ERR_ARG, "q and k must be %d-byte aligned", (int)al);
+    if (!aligned(lse, 4) || !aligned(weights, 4) || !aligned(prefix, 4))
+        return fail(DARD_ERR_ARG, "lse, weights and prefix must be 4-byte aligned");
+    const size_t need = dard_key_weights_workspace_bytes(dtype, b, R, Hq, Hkv, dh, P);
+    if (need && (!ws || ws_bytes < need)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", need);
+    if (need && !aligned(ws, 4)) return fail(DARD_ERR_ARG, "the workspace must be 4-byte aligned");
+    if (P == 0) return DARD_OK;
+    KeyWeightArgs a{};
+    a.q = q; a.lse = lse; a.k = k; a.prefix = prefix; a.weights = weights; a.ldw = ldw; a.part = (float*)ws;
+    a.P = P; a.cap = cap; a.b = b; a.R = R; a.Hq = Hq; a.Hkv = Hkv; a.dh = dh; a.scale = scale; a.decay = decay;
+    HIPOK(launch_key_weights(dtype, a, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+size_t dard_kv_select_workspace_bytes(int b, int Hkv, int P, int n) {
+    (void)b; (void)Hkv; (void)P; (void)n;
+    return 0;
+}
+
+dard_status dard_kv_select(const float* weights, int64_t ldw, int P, const int32_t* prefix, int b, int Hkv, int n, int first,
+                           int last, int32_t* keep, int32_t* kept, void* ws, size_t ws_bytes, void* stream) {
+    if (!weights || !keep) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (b < 1 || Hkv < 1 || P < 0 || n < 1 || ldw < P) return fail(DARD_ERR_SHAPE, "need b, Hkv, n >= 1 and 0 <= P <= ldw");
+    if (first < 0 || last < 0 || first > n || last > n - first)
+        return fail(DARD_ERR_SHAPE, "need first, last >= 0 and first + last <= n");
+    if ((double)b * Hkv >= 4194304.0 || (double)b * Hkv * n > 1099511627776.0) return fail(DARD_ERR_SHAPE, "too many heads in one call");
+    if (!aligned(weights, 4) || !aligned(prefix, 4) || !aligned(keep, 4) || !aligned(kept, 4))
+        return fail(DARD_ERR_ARG, "tensors must be 4-byte aligned");
+    (void)ws; (void)ws_bytes;
+    KvSelectArgs a{};
+    a.weights = weights; a.ldw = ldw; a.prefix = prefix; a.keep = keep; a.kept = kept;
+    a.b = b; a.Hkv = Hkv; a.P = P; a.n = n; a.first = first; a.last = last;
+    HIPOK(launch_kv_select(a, (hipStream_t)stream));
+    return DARD_OK;
+}
+
+dard_status dard_kv_compact(int dtype, void* k, void* v, int cap, float* weights, int64_t ldw, const int32_t* keep, int n,
+                            const int32_t* kept, int P, const int32_t* prefix, int b, int Hkv, int dh, void* stream) {
+    if (!k || !v || !keep) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (int rc = check_kv_type(dtype)) return rc;
+    if (int rc = check_heads(b, Hkv, Hkv, dh)) return rc;
+    if (P < 0 || n < 1 || P > cap || (weights && ldw < P)) return fail(DARD_ERR_SHAPE, "need n >= 1 and 0 <= P <= cap, ldw");
+    if ((double)b * Hkv > 524288.0) return fail(DARD_ERR_SHAPE, "too many heads in one call");
+    if (!aligned(k, kv_align(dtype)) || !aligned(v, dtype == DARD_DTYPE_F32 ? 4 : dtype == DARD_DTYPE_BF16 ? 2 : 1))
+        return fail(DARD_ERR_ARG, "k must be %d-byte aligned, v to its element", (int)kv_align(dtype));
+    if (!aligned(weights, 4) || !aligned(prefix, 4) || !aligned(keep, 4) || !aligned(kept, 4))
+        return fail(DARD_ERR_ARG, "weights, prefix, keep and kept must be 4-byte aligned");
+    if (P == 0) return DARD_OK;
+    KvCompactArgs a{};
+    a.k = k; a.v = v; a.weights = weights; a.ldw = ldw; a.prefix = prefix; a.keep = keep; a.kept = kept;
+    a.b = b; a.Hkv = Hkv; a.dh = dh; a.cap = cap; a.P = P; a.n = n;
+    HIPOK(launch_kv_compact(dtype, a, (hipStream_t)stream));
+    return DARD_OK;
+}
+
 // ---------------------------------------------------------------- weights / KV
 size_t dard_packed_weight_bytes(const dard_dims* dims) {
     if (check_dims(dims)) return 0;

@@ -1,0 +1,470 @@
+// Which keys of a cache get attention, and the cache cut to those that do:
+// the softmax weight of every key summed over the rows that read it
+// (dard_key_weights), the keys with the largest sums (dard_kv_select) and the
+// compaction of K, V and the sums to them (dard_kv_compact).  The prefix cache is
+// that of App. C.5.
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_tiles.h"
+#include "common.h"
+#include "launch.h"
+
+namespace dard {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ int prefix_len(const int32_t* prefix, int s, int P) {
+    return prefix ? min(max(prefix[s], 0), P) : P;
+}
+
+// ---------------------------------------------------------------- key weights
+// W_j = decay W_j + sum_r e^(scale q_r . k_j - L_r) over the rows r of all query
+// heads of the KV head, L_r the row's log softmax sum.
+//
+// S^T = K Q^T on v_mfma_f32_32x32x16_bf16 with the keys in registers (32 KB per
+// wave) and the rows streamed through LDS, 64 at a time, so a lane holds one row
+// and 16 KB keys: L_r is one register, a score costs a multiply-add, an exp2 and
+// an addition, and lanes are summed once, at the end.  Rows are split over
+// workgroups where keys alone are too few (partial sums in memory, added in
+// order).
+constexpr int kWRows = 64;       // rows of a stage
+
+// A workgroup's (sequence, KV head), key tile and row split: splits fastest, then
+// key tiles, dealt to the XCDs in contiguous runs, so those that read the same rows
+// share an L2.
+struct WeightUnit {
+    int head, kt, split;
+};
+__device__ __forceinline__ WeightUnit weight_unit(const KeyWeightArgs& a, int nsplit, int tile) {
+    const int total = gridDim.x, x = blockIdx.x & 7, ktiles = (a.P + tile - 1) / tile;
+    const int bid = x * (total >> 3) + min(x, total & 7) + (blockIdx.x >> 3);
+    return {bid / nsplit / ktiles, bid / nsplit % ktiles, bid % nsplit};
+}
+
+// decay = 0 does not read the old sum (it may hold anything).
+__device__ __forceinline__ void add_weight(const KeyWeightArgs& a, int head, int key, float x) {
+    float* w = a.weights + (size_t)head * a.ldw + key;
+    *w = a.decay == 0.f ? x : fmaf(a.decay, *w, x);
+}
+
+template <int DH, int KB, bool KV8>
+__global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int nsplit) {
+    constexpr int NC = DH / 16, CH = DH / 8;                 // MFMA steps; 16-byte chunks of a row
+    constexpr int STAGE = kWRows * DH * 2, NI = kWRows * CH / 256;
+    __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
+    typedef __attribute__((address_space(3))) void* lds_ptr;
+    typedef __attribute__((address_space(1))) void* glb_ptr;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lr = lane & 31, eta = lane >> 5;
+    const WeightUnit un = weight_unit(a, nsplit, 128 * KB);
+    const int g = un.head % a.Hkv, s = un.head / a.Hkv, kt = un.kt, split = un.split;
+    const int p = prefix_len(a.prefix, s, a.P), k0 = (kt * 4 + wave) * 32 * KB;
+    if (kt * 128 * KB >= p) return;
+    const int GQ = a.Hq / a.Hkv, rows = GQ * a.R;
+    const int ntile = (rows + kWRows - 1) / kWRows;
+    const int t0 = (int)((long long)ntile * split / nsplit), t1 = (int)((long long)ntile * (split + 1) / nsplit);
+
+    // rows in the order (position row, head): GQ neighbours in memory
+    const bf16_t* qb = reinterpret_cast<const bf16_t*>(a.q) + ((size_t)s * a.R * a.Hq + (size_t)g * GQ) * DH;
+    const float* lb = a.lse + (size_t)s * a.R * a.Hq + (size_t)g * GQ;
+    auto row_at = [&](int rho) __attribute__((always_inline)) { return (size_t)(rho / GQ) * a.Hq + rho % GQ; };
+    // chunk c of row r sits in slot c ^ swizzle(r): the operand reads of 16 lanes hit different banks
+    auto swz = [&](int r) __attribute__((always_inline)) { return CH == 16 ? r & 15 : (r ^ (r >> 3)) & 7; };
+    auto issue = [&](int t, char* dst) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int q = (wave * NI + j) * 64 + lane, r = q / CH, c = (q % CH) ^ swz(r);
+            const bf16_t* src = qb + row_at(min(t * kWRows + r, rows - 1)) * DH + 8 * c;
+            __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+        }
+    };
+    if (t0 < t1) issue(t0, smem);
+
+    // this wave's keys: A operand row lr of block kb; a key past the last one repeats it.
+    // Step c of an operand takes chunk ch(c, eta) of its row (any order will do that K and
+    // Q share; this one makes a lane's FP8 codes of two steps 16 neighbouring bytes)
+    auto ch = [&](int c) __attribute__((always_inline)) { return 4 * (c >> 1) + 2 * eta + (c & 1); };
+    bf16x8 kf[KB][NC];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        const size_t key = min(k0 + 32 * kb + lr, p - 1);
+        const size_t row = (((size_t)s * a.Hkv + g) * a.cap + key) * DH;
+        if constexpr (KV8) {
+#pragma unroll
+            for (int c = 0; c < NC; c += 2) {
+                const uint4 w = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(a.k) + row + 8 * ch(c));
+                kf[kb][c] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8(make_uint2(w.x, w.y)));
+                kf[kb][c + 1] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8(make_uint2(w.z, w.w)));
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kf[kb][c] = ld_bf16x8(reinterpret_cast<const bf16_t*>(a.k) + row + 8 * ch(c));
+        }
+    }
+    const float sl2 = a.scale * kLog2e;
+    float acc[KB][16];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[kb][v] = 0.f;
+
+    for (int t = t0; t < t1; ++t) {
+        char* cur = smem + ((t - t0) & 1) * STAGE;
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();                                     // stage t has arrived, and stage t - 1 is read
+        if (t + 1 < t1) issue(t + 1, smem + ((t + 1 - t0) & 1) * STAGE);
+#pragma unroll
+        for (int half = 0; half < kWRows / 32; ++half) {
+            const int rho = t * kWRows + 32 * half + lr;
+            const float L = rho < rows ? lb[row_at(rho)] : INFINITY;
+            const bool live = fabsf(L) < INFINITY || L != L; // (a row without a sum counts nothing; NaN stays NaN)
+            const float bias = -L * kLog2e;
+            bf16x8 qf[NC];
+            const int r = 32 * half + lr;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                qf[c] = *reinterpret_cast<const bf16x8*>(cur + 16 * (r * CH + (ch(c) ^ swz(r))));
+            const bool all = __all(live);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                floatx16 sc;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[v] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) sc = mfma32x32x16(kf[kb][c], qf[c], sc);
+                if (all) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[kb][v] += __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias));
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        acc[kb][v] += live ? __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias)) : 0.f;
+                }
+            }
+        }
+    }
+    // sum over the 32 lanes of a half: element v of block kb is key 32 kb + 8 (v / 4) + 4 eta + v % 4
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            float x = acc[kb][v];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+            const int key = k0 + 32 * kb + 8 * (v >> 2) + 4 * eta + (v & 3);
+            if (lr == v && key < p) {
+                if (nsplit > 1) a.part[((size_t)split * a.b * a.Hkv + un.head) * a.P + key] = x;
+                else add_weight(a, un.head, key, x);
+            }
+        }
+}
+
+// The same on v_mfma_f32_16x16x4_f32: a wave takes 32 keys, rows come straight from memory.
+template <int DH>
+__global__ __launch_bounds__(256) void key_weights_f32_kernel(KeyWeightArgs a, int nsplit) {
+    constexpr int NC = DH / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lr = lane & 15, q4 = lane >> 4;
+    const WeightUnit un = weight_unit(a, nsplit, 128);
+    const int g = un.head % a.Hkv, s = un.head / a.Hkv, kt = un.kt, split = un.split;
+    const int p = prefix_len(a.prefix, s, a.P), k0 = (kt * 4 + wave) * 32;
+    if (k0 >= p) return;
+    const int GQ = a.Hq / a.Hkv, rows = GQ * a.R, ntile = (rows + 15) / 16;
+    const int t0 = (int)((long long)ntile * split / nsplit), t1 = (int)((long long)ntile * (split + 1) / nsplit);
+    const float* qb = reinterpret_cast<const float*>(a.q) + ((size_t)s * a.R * a.Hq + (size_t)g * GQ) * DH;
+    const float* lb = a.lse + (size_t)s * a.R * a.Hq + (size_t)g * GQ;
+    floatx4 kf[2][NC];
+    float acc[2][4] = {};
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+            kf[kb][c] = ld_f4(reinterpret_cast<const float*>(a.k) +
+                              (((size_t)s * a.Hkv + g) * a.cap + min(k0 + 16 * kb + lr, p - 1)) * DH + 16 * c + 4 * q4);
+    for (int t = t0; t < t1; ++t) {
+        const int rho = t * 16 + lr, rc = min(rho, rows - 1);
+        const size_t at = (size_t)(rc / GQ) * a.Hq + rc % GQ;
+        const float L = rho < rows ? lb[at] : INFINITY;
+        const bool live = fabsf(L) < INFINITY || L != L;
+        floatx4 qf[NC], sc[2];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) qf[c] = ld_f4(qb + at * DH + 16 * c + 4 * q4);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            sc[kb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[kb] = mfma16x16x4f(kf[kb][c][e], qf[c][e], sc[kb]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                acc[kb][e] += live ? __builtin_amdgcn_exp2f((fmaf(sc[kb][e], a.scale, -L)) * kLog2e) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x = acc[kb][e];
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+            const int key = k0 + 16 * kb + 4 * q4 + e;
+            if (lr == 0 && key < p) {
+                if (nsplit > 1) a.part[((size_t)split * a.b * a.Hkv + un.head) * a.P + key] = x;
+                else add_weight(a, un.head, key, x);
+            }
+        }
+}
+
+// Partial sums of a row split, added in order.
+__global__ __launch_bounds__(256) void key_weights_sum_kernel(KeyWeightArgs a, int nsplit) {
+    const int blocks = (a.P + 255) / 256, head = blockIdx.x / blocks;
+    const int key = blockIdx.x % blocks * 256 + threadIdx.x;
+    if (key >= prefix_len(a.prefix, head / a.Hkv, a.P)) return;
+    float x = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < nsplit; ++i) x += a.part[((size_t)i * a.b * a.Hkv + head) * a.P + key];
+    add_weight(a, head, key, x);
+}
+
+struct WeightCfg {
+    int kb, ktiles, ns;
+};
+
+WeightCfg weight_cfg(int dtype, int b, int R, int Hq, int Hkv, int P) {
+    WeightCfg c{};
+    const long rows = (long)R * (Hq / Hkv), heads = (long)b * Hkv;
+    c.kb = dtype == DARD_DTYPE_F32 || heads * ((P + 255) / 256) < 512 ? 1 : 2;
+    c.ktiles = (P + 128 * c.kb - 1) / (128 * c.kb);
+    const long wgs = heads * c.ktiles, tiles = (rows + kWRows - 1) / kWRows;
+    c.ns = (int)std::max<long>(1, std::min<long>(512 / wgs, tiles / 4));
+    return c;
+}
+
+// ---------------------------------------------------------------- selection
+// The m = min(n, length) keys of a (sequence, KV head) row of sums that rank
+// highest: protected keys first, then by sum, ties to the lowest index.  Sums
+// map to unsigned integers of the same order (NaN below minus infinity, -0 as 0,
+// protected keys above all), and the rank's threshold is found digit by digit
+// from histograms in LDS.  One workgroup a row; each of its waves owns a run of
+// consecutive keys, counts what it keeps, and writes its indices behind those of
+// the waves before it.
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+
+__device__ __forceinline__ uint32_t sum_rank(float w) {
+    if (w != w) return 0u;
+    const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+    return (u >> 31) ? ~u : u | 0x80000000u;                 // -inf: 0x007FFFFF; +inf: 0xFF800000
+}
+
+__global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) {
+    __shared__ uint32_t hist[2048];
+    __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
+    __shared__ uint32_t found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int s = blockIdx.x / a.Hkv;
+    const int p = prefix_len(a.prefix, s, a.P), m = min(a.n, p);
+    const float* w = a.weights + (size_t)blockIdx.x * a.ldw;
+    int32_t* keep = a.keep + (size_t)blockIdx.x * a.n;
+    if (a.kept && blockIdx.x % a.Hkv == 0 && tid == 0) a.kept[s] = m;
+    for (int i = m + tid; i < a.n; i += kSelThreads) keep[i] = -1;
+    if (m == p) {                                            // nothing to leave out
+        for (int i = tid; i < m; i += kSelThreads) keep[i] = i;
+        return;
+    }
+    auto rank = [&](int j) __attribute__((always_inline)) {
+        return j < a.first || j >= p - a.last ? 0xFFFFFFFFu : sum_rank(w[j]);
+    };
+    // threshold T: fewer than m keys rank above it, m or more at or above it
+    uint32_t T = 0, mask = 0;
+    int need = m;                                            // keys to take among those that agree with T under mask
+    constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
+#pragma unroll
+    for (int d = 0; d < 3; ++d) {
+        for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < p; j += kSelThreads) {
+            const uint32_t u = rank(j);
+            if ((u & mask) == T) atomicAdd(&hist[(u >> kShift[d]) & ((1u << kBits[d]) - 1)], 1u);
+        }
+        __syncthreads();
+        // the bin in which the count from the top passes need (integer counts: order plays no part)
+        uint32_t c0 = hist[2047 - 2 * tid], c1 = hist[2046 - 2 * tid];   // this thread's two bins, from the top
+        uint32_t run = c0 + c1;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t below = __shfl_up(run, o, 64);
+            if (lane >= o) run += below;
+        }
+        if (lane == 63) wsum[wave] = run;
+        __syncthreads();
+        uint32_t before = run - c0 - c1;
+        for (int i = 0; i < wave; ++i) before += wsum[i];
+        const uint32_t want = (uint32_t)need;
+        if (before < want && before + c0 >= want) { found[0] = 2047 - 2 * tid; found[1] = before; }
+        if (before + c0 < want && before + c0 + c1 >= want) { found[0] = 2046 - 2 * tid; found[1] = before + c0; }
+        __syncthreads();
+        T |= found[0] << kShift[d];
+        mask |= ((1u << kBits[d]) - 1) << kShift[d];
+        need -= (int)found[1];
+    }
+    // keys above T, and the first `need` of those that equal it, in index order
+    const int per = ((p + kSelWaves - 1) / kSelWaves + 63) / 64 * 64, j0 = wave * per, j1 = min(p, j0 + per);
+    uint32_t above = 0, ties = 0;
+    for (int j = j0; j < j1; j += 64) {
+        const uint32_t u = j + lane < j1 ? rank(j + lane) : 0u;
+        const bool in = j + lane < j1;
+        above += __builtin_popcountll(__ballot(in && u > T));
+        ties += __builtin_popcountll(__ballot(in && u == T));
+    }
+    if (lane == 0) { wsum[wave] = above; wtie[wave] = ties; }
+    __syncthreads();
+    uint32_t pos = 0, tie = 0;                               // keys above T, and ties, before this wave's run
+    for (int i = 0; i < wave; ++i) { pos += wsum[i]; tie += wtie[i]; }
+    const uint64_t lower = (1ull << lane) - 1;
+    for (int j = j0; j < j1; j += 64) {
+        const bool in = j + lane < j1;
+        const uint32_t u = in ? rank(j + lane) : 0u;
+        const uint64_t ba = __ballot(in && u > T), bt = __ballot(in && u == T);
+        const uint32_t my_tie = tie + __builtin_popcountll(bt & lower);
+        const bool take = in && (u > T || (u == T && my_tie < (uint32_t)need));
+        const uint32_t at = pos + __builtin_popcountll(ba & lower) + min(my_tie, (uint32_t)need);
+        if (take) keep[at] = j + lane;
+        pos += __builtin_popcountll(ba);
+        tie += __builtin_popcountll(bt);
+    }
+}
+
+// ---------------------------------------------------------------- compaction
+// Key j of a (sequence, KV head) becomes key keep[j], in place.  keep ascends, so
+// keep[j] >= j: chunk by chunk a workgroup reads the sources of a run of places,
+// then writes that run, which no later chunk reads.  A workgroup owns whole
+// columns (a run of a key's bytes, or rows of the dims-major V), so the order of
+// reads and writes is its own affair.
+constexpr int kMoveThreads = 256;
+
+// K: a workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time.
+template <int SEG>
+__device__ void move_keys(char* k, int row_bytes, const int32_t* keep, int m, int P) {
+    constexpr int LPR = SEG / 16, STEP = kMoveThreads / LPR, U = 8;   // lanes a key, keys a pass, passes in flight
+    const int tid = threadIdx.x, key = tid / LPR, at = tid % LPR * 16;
+    for (int j0 = 0; j0 < m; j0 += U * STEP) {
+        uint4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * STEP + key;
+            if (j < m) x[u] = *reinterpret_cast<const uint4*>(k + (size_t)min(max(keep[j], 0), P - 1) * row_bytes + at);
+        }
+        __builtin_amdgcn_s_waitcnt(0);                       // (every source is in registers)
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * STEP + key;
+            if (j < m) *reinterpret_cast<uint4*>(k + (size_t)j * row_bytes + at) = x[u];
+        }
+    }
+}
+
+// V: a workgroup owns ROWS dims; a thread moves elements of all of them.
+template <typename T, int ROWS>
+__device__ void move_values(T* v, int cap, const int32_t* keep, int m, int P) {
+    constexpr int U = 4;
+    const int tid = threadIdx.x;
+    for (int j0 = 0; j0 < m; j0 += U * kMoveThreads) {
+        T x[U][ROWS];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * kMoveThreads + tid;
+            if (j < m) {
+                const int src = min(max(keep[j], 0), P - 1);
+#pragma unroll
+                for (int d = 0; d < ROWS; ++d) x[u][d] = v[(size_t)d * cap + src];
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * kMoveThreads + tid;
+            if (j < m) {
+#pragma unroll
+                for (int d = 0; d < ROWS; ++d) v[(size_t)d * cap + j] = x[u][d];
+            }
+        }
+    }
+}
+
+// Grid: x = parts of a (sequence, KV head): DH bytes-of-K segments, then groups of V rows,
+// then (with sums) one part for them; parts fastest.
+template <typename T, int DH>
+__global__ __launch_bounds__(kMoveThreads) void kv_compact_kernel(KvCompactArgs a) {
+    constexpr int SEG = 64, ROWS = 8, KP = DH * (int)sizeof(T) / SEG, VP = DH / ROWS;
+    const int parts = KP + VP + (a.weights ? 1 : 0), head = blockIdx.x / parts, s = head / a.Hkv;
+    const int p = prefix_len(a.prefix, s, a.P);
+    const int m = min(a.kept ? max(a.kept[s], 0) : a.n, min(a.n, p));
+    const int32_t* keep = a.keep + (size_t)head * a.n;
+    const size_t base = (size_t)head * a.cap * DH;
+    int part = blockIdx.x % parts;
+    if (part < KP) {
+        move_keys<SEG>(reinterpret_cast<char*>(a.k) + base * sizeof(T) + part * SEG, DH * sizeof(T), keep, m, max(p, 1));
+        return;
+    }
+    part -= KP;
+    if (part < VP) {
+        move_values<T, ROWS>(reinterpret_cast<T*>(a.v) + base + (size_t)part * ROWS * a.cap, a.cap, keep, m, max(p, 1));
+        return;
+    }
+    float* w = a.weights + (size_t)head * a.ldw;
+    move_values<float, 1>(w, 0, keep, m, max(p, 1));
+    __syncthreads();
+    for (int j = m + threadIdx.x; j < p; j += kMoveThreads) w[j] = 0.f;   // freed places start from nothing
+}
+
+}  // namespace
+
+size_t key_weights_partial_floats(int dtype, int b, int R, int Hq, int Hkv, int P) {
+    const WeightCfg c = weight_cfg(dtype, b, R, Hq, Hkv, P);
+    return c.ns <= 1 ? 0 : (size_t)c.ns * b * Hkv * P;
+}
+
+hipError_t launch_key_weights(int dtype, const KeyWeightArgs& a, hipStream_t s) {
+    const WeightCfg c = weight_cfg(dtype, a.b, a.R, a.Hq, a.Hkv, a.P);
+    const dim3 grid((unsigned)((long)a.b * a.Hkv * c.ktiles * c.ns));
+    void (*k)(KeyWeightArgs, int);
+    if (dtype == DARD_DTYPE_F32) k = a.dh == 128 ? key_weights_f32_kernel<128> : key_weights_f32_kernel<64>;
+    else if (dtype == DARD_DTYPE_BF16_KV_FP8)
+        k = a.dh == 128 ? (c.kb == 2 ? key_weights_kernel<128, 2, true> : key_weights_kernel<128, 1, true>)
+                        : (c.kb == 2 ? key_weights_kernel<64, 2, true> : key_weights_kernel<64, 1, true>);
+    else
+        k = a.dh == 128 ? (c.kb == 2 ? key_weights_kernel<128, 2, false> : key_weights_kernel<128, 1, false>)
+                        : (c.kb == 2 ? key_weights_kernel<64, 2, false> : key_weights_kernel<64, 1, false>);
+    launch(k, grid, dim3(256), 0, s, a, c.ns);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || c.ns == 1) return e;
+    launch(key_weights_sum_kernel, dim3((unsigned)((long)a.b * a.Hkv * ((a.P + 255) / 256))), dim3(256), 0, s, a, c.ns);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s) {
+    launch(kv_select_kernel, dim3(a.b * a.Hkv), dim3(kSelThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t compact(const KvCompactArgs& a, hipStream_t s) {
+    const int parts = a.dh * (int)sizeof(T) / 64 + a.dh / 8 + (a.weights ? 1 : 0);
+    const dim3 grid((unsigned)((long)parts * a.b * a.Hkv));
+    if (a.dh == 128) launch(kv_compact_kernel<T, 128>, grid, dim3(kMoveThreads), 0, s, a);
+    else launch(kv_compact_kernel<T, 64>, grid, dim3(kMoveThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_compact(int dtype, const KvCompactArgs& a, hipStream_t s) {
+    if (dtype == DARD_DTYPE_F32) return compact<float>(a, s);
+    return dtype == DARD_DTYPE_BF16 ? compact<bf16_t>(a, s) : compact<uint8_t>(a, s);
+}
+
+}  // namespace dard

@@ -60,6 +60,53 @@ int attention_tiles(int masked, int P, int B, int nkeys);
 size_t attention_partial_slots(int dtype, int b, int R, int Hq, int Hkv, int ntiles);
 hipError_t launch_attention(int dtype, const AttnArgs& a, hipStream_t s);
 
+// ---- shared_attention.hip
+struct SharedAttnArgs {
+    const void* q; void* out;             // [b][2B][Hq][dh]
+    float* lse;                           // [b][2B][Hq], or NULL
+    const void* ksh; const void* vsh;     // [Hkv][cap_sh][dh], [Hkv][dh][cap_sh]: keys 0 .. Ps - 1 of every sequence
+    const void* k; const void* v;         // [b][Hkv][cap][dh], [b][Hkv][dh][cap]: own prefix, then the block
+    const uint8_t* state; const float* conf;   // [b][B] (fp32)
+    const uint64_t* sel;                  // [b][2B][ceil(B / 64)] take-x words (bf16)
+    const int32_t* prefix;                // [b] own prefix lengths (clamped to [0, P]), or NULL: P
+    int Ps, cap_sh, P, cap, b, B, Hq, Hkv, dh;
+    float scale;
+    uint32_t flags;
+    float* part;                          // key-split partials (shared_attention_partial_floats)
+};
+size_t shared_attention_partial_floats(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P);
+hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, hipStream_t s);
+
+// ---- evict.hip
+struct KeyWeightArgs {
+    const void* q; const float* lse;      // [b][R][Hq][dh], [b][R][Hq]
+    const void* k;                        // [b][Hkv][cap][dh]
+    const int32_t* prefix;                // [b] lengths (clamped to [0, P]), or NULL: P
+    float* weights;                       // [b][Hkv] rows of P sums, ldw apart
+    int64_t ldw;
+    float* part;                          // row-split partial sums (key_weights_partial_floats)
+    int P, cap, b, R, Hq, Hkv, dh;
+    float scale, decay;
+};
+size_t key_weights_partial_floats(int dtype, int b, int R, int Hq, int Hkv, int P);
+hipError_t launch_key_weights(int dtype, const KeyWeightArgs& a, hipStream_t s);
+struct KvSelectArgs {
+    const float* weights;                 // [b][Hkv] rows, ldw apart
+    int64_t ldw;
+    const int32_t* prefix;
+    int32_t* keep; int32_t* kept;         // [b][Hkv][n], [b] or NULL
+    int b, Hkv, P, n, first, last;
+};
+hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s);
+struct KvCompactArgs {
+    void* k; void* v;                     // [b][Hkv][cap][dh], [b][Hkv][dh][cap]
+    float* weights;                       // [b][Hkv] rows, ldw apart, or NULL
+    int64_t ldw;
+    const int32_t* prefix; const int32_t* keep; const int32_t* kept;
+    int b, Hkv, dh, cap, P, n;
+};
+hipError_t launch_kv_compact(int dtype, const KvCompactArgs& a, hipStream_t s);
+
 // ---- gemm.hip
 enum EpiKind { EPI_STORE_F32 = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_QKV = 3, EPI_PARTIAL = 4, EPI_LMHEAD = 5 };
 

@@ -1,0 +1,830 @@
+// State-masked attention of a batch whose sequences share a prefix (Sec. 3.1,
+// Sec. 3.2; the prefix caching of App. C.5 for a prompt that a whole batch has).
+//
+// out_r = sum_k e^(s_rk - L_r) v_k,  L_r = log sum_k e^(s_rk),  s_rk = scale q_r . k_k
+// over the Ps shared keys, the keys of the row's own sequence, and of its block
+// the keys that the state mask lets it see.  The softmax is taken in one pass
+// with a running maximum and sum.
+//
+// The rows of all sequences and of all query heads of a KV head are one row
+// space, sequence by sequence, so a tile of shared keys that a workgroup stages
+// in LDS serves rows of as many sequences as fit: one position a sequence (two
+// rows) fills matrix tiles that a launch per sequence would leave empty, and the
+// shared keys are read once for 128 rows instead of once for two.  A workgroup
+// takes 32 WAVES consecutive rows and walks the shared tiles, then the own tiles
+// of each sequence among its rows; waves without rows of that sequence leave the
+// tile out.  An own tile is 64 consecutive keys of a sequence's prefix and
+// block, and one 64-bit word per row says which of them the row sees.
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_tiles.h"
+#include "common.h"
+#include "launch.h"
+
+namespace dard {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// The running maximum (log2 units) before a row has seen a score.  Any score
+// that float32 holds lies above it or makes exp2 of the difference infinite, so
+// a first tile always moves it; a hidden key's minus infinity still gives 0.
+constexpr float kLeast = -3.402823466e38f;
+constexpr float kBig = 256.f;        // a lane's probability sum over a tile that moves the running maximum
+constexpr int kMaxSplit = 32;        // key splits across workgroups
+
+// LDS of one group of TPG threads: three K stages [64 keys][DH] and two V^T
+// stages [DH][64 keys], or, at the end, every lane's o, m and l.
+template <int DH, int TPG>
+struct SLds {
+    static constexpr int TILE = kKeys * DH * 2;
+    static constexpr int MERGE = (DH / 2 + 2) * TPG * 4;
+    static constexpr int GROUP = ((5 * TILE > MERGE ? 5 * TILE : MERGE) + 15) / 16 * 16;
+};
+
+// A tile of the walk: seq < 0 for shared keys, else the sequence (counted from
+// the workgroup's first); keys k0 .. k0 + n - 1 of that cache; p the sequence's
+// prefix length.  Uniform over a workgroup's group.
+struct Tile {
+    int seq, k0, n, p;
+};
+
+// The block keys among keys k0 .. k0 + 63 of a sequence with prefix p that a row
+// with take-x words x sees, and every prefix key among them.
+__device__ __forceinline__ uint64_t own_word(const uint64_t (&x)[kBlockWords], int B, int p, int k0) {
+    const int s = k0 - p;                                    // block position of the tile's first key
+    const uint64_t pre = s >= 0 ? 0ull : (s <= -64 ? ~0ull : (1ull << -s) - 1);
+    return pre | bits64(x, B, s) | (~bits64(x, B, s - B) & range_mask(s - B, B));
+}
+
+template <int DH, int WAVES, int G, bool KV8>
+__global__ __launch_bounds__(64 * WAVES * G) __attribute__((amdgpu_waves_per_eu(2)))
+void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
+    constexpr int TPG = 64 * WAVES, ROWS = 32 * WAVES;
+    constexpr int NCH = kKeys * DH / 8, NI = NCH / TPG;      // 16-byte chunks of a tile, and of a thread
+    static_assert(NCH % TPG == 0 && ROWS <= 128, "whole chunks per thread; at most 64 sequences among the rows");
+    using L = SLds<DH, TPG>;
+    using KVT = typename std::conditional<KV8, uint8_t, bf16_t>::type;
+    typedef __attribute__((address_space(3))) void* lds_ptr;
+    typedef __attribute__((address_space(1))) void* glb_ptr;
+    __shared__ __attribute__((aligned(16))) char smem[G * L::GROUP];
+
+    const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / TPG), tid = threadIdx.x % TPG;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lr = lane & 31, eta = lane >> 5;
+    // row tile fastest, then key split, then KV head, dealt to the XCDs in
+    // contiguous runs: workgroups that read the same keys share an L2
+    int bid = blockIdx.x;
+    {
+        const int total = gridDim.x, per = total >> 3, more = total & 7, x = bid & 7;
+        bid = x * per + min(x, more) + (bid >> 3);
+    }
+    const int rt = bid % rowtiles, split = bid / rowtiles % nsplit, kvh = bid / rowtiles / nsplit;
+    const int GQ = a.Hq / a.Hkv, R = 2 * a.B, RS = GQ * R;   // rows of a sequence: (position row, head), head fastest
+    const int total_rows = a.b * RS;
+
+    // ---- the walk: shared tiles, then the own tiles of sequences s0 ..; lane i
+    // holds the prefix length of sequence s0 + i and the own tiles up to it
+    const int s0 = rt * ROWS / RS;
+    const int nseq = (min(rt * ROWS + ROWS, total_rows) - 1) / RS - s0 + 1;   // at most 64: RS >= 2 and ROWS <= 128
+    const int nsh = (a.Ps + kKeys - 1) / kKeys;
+    int plen = 0, upto = 0;
+    if (lane < nseq) {
+        plen = a.prefix ? min(max(a.prefix[s0 + lane], 0), a.P) : a.P;
+        upto = (plen + R + kKeys - 1) / kKeys;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int below = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += below;
+    }
+    const int ntiles = nsh + __builtin_amdgcn_readlane(upto, 63);
+    const int t_begin = (int)((long long)ntiles * split / nsplit), t_end = (int)((long long)ntiles * (split + 1) / nsplit);
+    const int iters = (t_end - t_begin + G - 1) / G;
+    auto tile_at = [&](int t) __attribute__((always_inline)) {
+        Tile d;
+        if (t < nsh) {
+            d.seq = -1;
+            d.k0 = t * kKeys;
+            d.n = min(kKeys, a.Ps - d.k0);
+            d.p = 0;
+        } else {
+            const int u = t - nsh;
+            const int i = __builtin_popcountll(__ballot(upto <= u));   // (lanes past the last sequence hold the total)
+            d.seq = i;
+            d.p = __builtin_amdgcn_readlane(plen, i);
+            d.k0 = (u - (i ? __builtin_amdgcn_readlane(upto, i - 1) : 0)) * kKeys;
+            d.n = min(kKeys, d.p + R - d.k0);
+        }
+        return d;
+    };
+    auto mine = [&](int it) __attribute__((always_inline)) { return t_begin + grp + G * it < t_end; };
+    auto at = [&](int it) __attribute__((always_inline)) { return tile_at(t_begin + grp + G * it); };
+
+    const KVT* ksh = reinterpret_cast<const KVT*>(a.ksh) + (size_t)kvh * a.cap_sh * DH;
+    const KVT* vsh = reinterpret_cast<const KVT*>(a.vsh) + (size_t)kvh * a.cap_sh * DH;
+    char* gbase = smem + grp * L::GROUP;
+    auto keys_of = [&](const Tile& d) __attribute__((always_inline)) {
+        const KVT* base = d.seq < 0 ? ksh : reinterpret_cast<const KVT*>(a.k) + ((size_t)(s0 + d.seq) * a.Hkv + kvh) * a.cap * DH;
+        return base + (size_t)d.k0 * DH;
+    };
+    auto values_of = [&](const Tile& d) __attribute__((always_inline)) {
+        const KVT* base = d.seq < 0 ? vsh : reinterpret_cast<const KVT*>(a.v) + ((size_t)(s0 + d.seq) * a.Hkv + kvh) * a.cap * DH;
+        return base + d.k0;
+    };
+
+    // ---- copies into LDS.  Chunk q = (wave NI + j) 64 + lane of the swizzled
+    // image goes straight there (16 bytes a lane; an FP8 cache goes through
+    // registers and is widened).  Nothing past a tile's n keys is read: K rows past
+    // them are left out (their scores are masked, whatever the stage held), V
+    // chunks past them are zeros, a chunk that straddles n is put together by
+    // elements.
+    auto krc = [&](int j, int& r, int& c) __attribute__((always_inline)) {
+        const int q = (wave * NI + j) * 64 + lane;
+        r = q / (DH / 8);
+        c = (q % (DH / 8)) ^ kswz<DH>(r);
+    };
+    auto vrc = [&](int j, int& d, int& c) __attribute__((always_inline)) {
+        const int q = (wave * NI + j) * 64 + lane;
+        d = q / (kKeys / 8);
+        c = (q % (kKeys / 8)) ^ vswz(d);
+    };
+    uint2 kreg[NI], vreg[NI];
+    auto load_k8 = [&](const Tile& t) __attribute__((always_inline)) {
+        const KVT* kt = keys_of(t);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            int r, c;
+            krc(j, r, c);
+            if (r < t.n) kreg[j] = *reinterpret_cast<const uint2*>(kt + r * DH + 8 * c);
+        }
+    };
+    auto commit_k8 = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            int r, c;
+            krc(j, r, c);
+            if (r < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(kreg[j]);
+        }
+    };
+    auto load_v8 = [&](const Tile& t) __attribute__((always_inline)) {
+        const KVT* vt = values_of(t);
+        const int vcap = t.seq < 0 ? a.cap_sh : a.cap;
+        // (rows of 8-byte chunks that are all aligned: the usual case)
+        if (t.n == kKeys && ((vcap | (int)reinterpret_cast<uintptr_t>(vt)) & 7) == 0) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                int d, c;
+                vrc(j, d, c);
+                vreg[j] = *reinterpret_cast<const uint2*>(vt + (size_t)d * vcap + 8 * c);
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            int d, c;
+            vrc(j, d, c);
+            const KVT* src = vt + (size_t)d * vcap + 8 * c;
+            const int cnt = t.n - 8 * c;                     // keys of the chunk inside the tile
+            uint2 w = make_uint2(0u, 0u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < cnt) {
+                    const uint32_t bt = (uint32_t)src[e] << (8 * (e & 3));
+                    if (e < 4) w.x |= bt; else w.y |= bt;
+                }
+            vreg[j] = w;
+        }
+    };
+    auto commit_v8 = [&](char* dst) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+            *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(vreg[j]);
+    };
+    auto issue_k = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
+        if constexpr (KV8) {
+            load_k8(t);
+            commit_k8(t, dst);
+        } else {
+            const KVT* kt = keys_of(t);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                int r, c;
+                krc(j, r, c);
+                if (t.n == kKeys || r < t.n)
+                    __builtin_amdgcn_global_load_lds((glb_ptr)(kt + r * DH + 8 * c), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+            }
+        }
+    };
+    auto issue_v = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
+        if constexpr (KV8) {
+            load_v8(t);
+            commit_v8(dst);
+        } else {
+            const KVT* vt = values_of(t);
+            const int vcap = t.seq < 0 ? a.cap_sh : a.cap;
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                int d, c;
+                vrc(j, d, c);
+                const KVT* src = vt + (size_t)d * vcap + 8 * c;
+                if (t.n == kKeys || 8 * c + 8 <= t.n) {
+                    __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+                } else {
+                    bf16x8 w = {};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (8 * c + e < t.n) w[e] = __builtin_bit_cast(__bf16, src[e]);
+                    *reinterpret_cast<bf16x8*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = w;
+                }
+            }
+        }
+    };
+    auto kst = [&](int i) __attribute__((always_inline)) { return gbase + (i % 3) * L::TILE; };
+    auto vst = [&](int i) __attribute__((always_inline)) { return gbase + (3 + (i & 1)) * L::TILE; };
+    if (mine(0)) {
+        issue_k(at(0), kst(0));
+        issue_v(at(0), vst(0));
+    }
+
+    // ---- this lane's query row, its Q operand and its take-x words
+    const int rho = rt * ROWS + 32 * wave + lr;
+    const bool row_ok = rho < total_rows;
+    const int rc = min(rho, total_rows - 1);
+    const int seq = rc / RS, r = rc % RS / GQ, h = kvh * GQ + rc % GQ;
+    const size_t orow = ((size_t)seq * R + r) * a.Hq + h;    // (sequence, row, head)
+    // sequences of the wave's rows, counted from s0 (a wave past the last row has none)
+    const int w_lo = __builtin_amdgcn_readfirstlane(seq) - s0, w_hi = __builtin_amdgcn_readlane(seq, 31) - s0;
+    const bool w_any = rt * ROWS + 32 * wave < total_rows;
+    bf16x8 qf[DH / 16];
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c)
+        qf[c] = ld_bf16x8(reinterpret_cast<const bf16_t*>(a.q) + orow * DH + 16 * c + 8 * eta);
+    // take-x words, read where a tile has block keys (they would hold 8 registers through the loop)
+    const int W = (a.B + 63) / 64;
+    const uint64_t* sel = a.sel + ((size_t)seq * R + r) * W;
+    const float sl2 = a.scale * kLog2e;
+    // K row pi(lr) of each 32-key block, V^T row lr: operand addresses inside a
+    // stage; a chunk or a block of rows further is an XOR or an offset
+    const uint32_t kaddr0 = 16 * kslot<DH>(swap23(lr), eta), vaddr0 = 16 * vslot(lr, eta);
+
+    floatx16 o[DH / 32];
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
+    float m_run = kLeast, l_run = 0.f;
+
+    // S^T = K Q^T: value v of block kb is key 32 kb + 16 (v / 8) + 8 eta + v % 8
+    auto scores = [&](const char* ks, floatx16 (&sc)[2]) __attribute__((always_inline)) {
+        constexpr int NC = DH / 16;
+        const uint32_t kb0 = (uint32_t)(ks - smem) + kaddr0;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            bf16x8 kf[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                kf[c] = *reinterpret_cast<const bf16x8*>(smem + ((kb0 ^ (32u * c)) + kb * 32 * DH * 2));
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) sc[kb] = mfma32x32x16(kf[c], qf[c], sc[kb]);
+            __builtin_amdgcn_sched_group_barrier(0x100, NC, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, NC, 0);
+        }
+    };
+    auto vfrag = [&](const char* vs, int d, int st) __attribute__((always_inline)) {
+        const uint32_t vb0 = (uint32_t)(vs - smem) + vaddr0;
+        return *reinterpret_cast<const bf16x8*>(smem + ((vb0 ^ (32u * (st ^ (2 * (d & 1))))) + d * 32 * kKeys * 2));
+    };
+    // mask, online softmax and O^T += V^T P^T.  Probabilities are taken against the
+    // running maximum as it stands, and once more against the tile's where a lane's
+    // sum of them passes kBig (or is NaN).  They are rounded to bf16 for the matrix
+    // unit (2^-8 of each at most); their sum is not.
+    auto softmax_pv = [&](floatx16 (&sc)[2], const Tile& t, const char* vs) __attribute__((always_inline)) {
+        // whole: every row of the wave sees every key of the tile
+        const bool whole = t.n == kKeys && (t.seq < 0 || (w_lo == w_hi && t.k0 + kKeys <= t.p));
+        uint64_t vis = ~0ull;
+        if (!whole) {
+            if (t.seq < 0) vis = (1ull << t.n) - 1;          // (n < 64 here)
+            else {
+                uint64_t xw[kBlockWords];
+#pragma unroll
+                for (int q = 0; q < kBlockWords; ++q) xw[q] = q < W ? sel[q] : 0ull;
+                vis = seq - s0 == t.seq ? own_word(xw, a.B, t.p, t.k0) : 0ull;
+            }
+            const uint64_t ww = vis >> (8 * eta);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (!((ww >> (32 * kb + 16 * (v >> 3) + (v & 7))) & 1ull)) sc[kb][v] = -INFINITY;
+        }
+        float psum = 0.f;
+        bf16x8 pb[2][2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[kb][v], sl2, -m_run));
+                psum += p;
+                pb[kb][v >> 3][v & 7] = (__bf16)p;
+            }
+        if (__ballot(!(psum <= kBig))) {
+            float mt = sc[0][0];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mt = fmaxf(mt, sc[kb][v]);
+            mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+            const float m_new = fmaxf(m_run, mt * sl2);      // sl2 > 0: the maximum commutes with the scale
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d) o[d] *= alpha;
+            l_run *= alpha;
+            m_run = m_new;
+            psum = 0.f;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(sc[kb][v], sl2, -m_run));
+                    psum += p;
+                    pb[kb][v >> 3][v & 7] = (__bf16)p;
+                }
+        }
+        l_run += psum;
+        if (!whole) {
+            // An infinity or NaN among the values of a tile that not every row sees
+            // whole must not reach the rows that do not see its key (0 times it is
+            // NaN): such elements leave the product and are added row by row.
+            uint32_t top = 0;
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const uint4 w = __builtin_bit_cast(uint4, vfrag(vs, d, st));
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        top |= ((u[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;   // exponent all ones
+                }
+            if (__ballot(top != 0)) {
+#pragma unroll
+                for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {
+                        bf16x8 f = vfrag(vs, d, st);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if ((__builtin_bit_cast(uint16_t, (__bf16)f[e]) & 0x7F80u) == 0x7F80u) f[e] = (__bf16)0.f;
+                        o[d] = mfma32x32x16(f, pb[st >> 1][st & 1], o[d]);
+                    }
+                for (int key = 0; key < t.n; ++key) {
+                    // the row's probability of this key, from the lane of the row that holds it
+                    const int kb = key >> 5, e = (key & 7) + 8 * ((key >> 4) & 1), from = lr + 32 * ((key >> 3) & 1);
+                    float pk = 0.f;
+#pragma unroll
+                    for (int b2 = 0; b2 < 2; ++b2)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            if (b2 == kb && v == e) pk = (float)pb[b2][v >> 3][v & 7];
+                    pk = __shfl(pk, from, 64);
+                    const bool sees = (vis >> key) & 1ull;
+#pragma unroll
+                    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int dim = 32 * d + 8 * (v >> 2) + 4 * eta + (v & 3);
+                            const bf16_t w = *reinterpret_cast<const bf16_t*>(vs + 16 * vslot(dim, key >> 3) + 2 * (key & 7));
+                            if (sees && (w & 0x7F80u) == 0x7F80u) o[d][v] += pk * bf2f(w);
+                        }
+                }
+                return;
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d) {
+            bf16x8 vf[4];
+#pragma unroll
+            for (int st = 0; st < 4; ++st) vf[st] = vfrag(vs, d, st);
+#pragma unroll
+            for (int st = 0; st < 4; ++st) o[d] = mfma32x32x16(vf[st], pb[st >> 1][st & 1], o[d]);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        }
+    };
+    // rows of this wave that the tile can concern
+    auto concerns = [&](const Tile& t) __attribute__((always_inline)) {
+        return w_any && (t.seq < 0 || (t.seq >= w_lo && t.seq <= w_hi));
+    };
+
+    // ---- main loop: V one step ahead of its use, K two (three for a second group,
+    // which runs half a step out of phase so that on every SIMD one wave's matrix
+    // instructions meet the other's softmax).  A step ends by waiting for every
+    // copy but the newest K tile's and publishing them with the barrier, which also
+    // retires every wave's reads of the stages that the next step overwrites.
+    // Copies complete in order, so V goes first; a ragged K tile issues fewer
+    // copies than the count assumes, so then all are waited for.
+    const bool late = G > 1 && grp == 1;
+    if (mine(1)) issue_k(at(1), kst(1));
+    if (late && mine(2)) issue_k(at(2), kst(2));
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    const int lead = late ? 3 : 2;
+    floatx16 sc[2];
+    if constexpr (G > 1) {
+        if (late) {
+            if (mine(0)) {
+                const Tile t = at(0);
+                if (concerns(t)) scores(kst(0), sc);
+            }
+            // (K tile 3 goes over the stage that these scores read)
+            __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
+        }
+        wg_barrier();
+    }
+    for (int it = 0; it < iters; ++it) {
+        const bool nextv = mine(it + 1), ahead = mine(it + lead);
+        Tile tv = {}, tk = {};
+        if (nextv) {
+            tv = at(it + 1);
+            if constexpr (KV8) load_v8(tv); else issue_v(tv, vst(it + 1));
+        }
+        if (ahead) {
+            tk = at(it + lead);
+            if constexpr (KV8) load_k8(tk); else issue_k(tk, kst(it + lead));
+        }
+        if (!late) {
+            if (mine(it)) {
+                const Tile t = at(it);
+                if (concerns(t)) {
+                    scores(kst(it), sc);
+                    softmax_pv(sc, t, vst(it));
+                }
+            }
+        } else {
+            if (mine(it)) {
+                const Tile t = at(it);
+                if (concerns(t)) softmax_pv(sc, t, vst(it));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (nextv && concerns(tv)) scores(kst(it + 1), sc);
+        }
+        if constexpr (KV8) {
+            if (nextv) commit_v8(vst(it + 1));
+            if (ahead) commit_k8(tk, kst(it + lead));
+            __builtin_amdgcn_s_waitcnt(0);
+        } else {
+            if (ahead && tk.n == kKeys) __builtin_amdgcn_s_waitcnt(waitcnt_vm(NI));
+            else __builtin_amdgcn_s_waitcnt(0);
+        }
+        wg_barrier();
+    }
+
+    // ---- merge the groups through LDS (group 0 keeps the result)
+    if constexpr (G > 1) {
+        float* mb = reinterpret_cast<float*>(gbase);
+        if (grp > 0) {
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mb[(16 * d + v) * TPG + tid] = o[d][v];
+            mb[(DH / 2) * TPG + tid] = m_run;
+            mb[(DH / 2 + 1) * TPG + tid] = l_run;
+        }
+        __syncthreads();
+        if (grp > 0) return;
+#pragma unroll
+        for (int gg = 1; gg < G; ++gg) {
+            const float* ob = reinterpret_cast<const float*>(smem + gg * L::GROUP);
+            const float m2 = ob[(DH / 2) * TPG + tid], M = fmaxf(m_run, m2);
+            const float f0 = __builtin_amdgcn_exp2f(m_run - M), f1 = __builtin_amdgcn_exp2f(m2 - M);
+            l_run = l_run * f0 + ob[(DH / 2 + 1) * TPG + tid] * f1;
+            m_run = M;
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[d][v] = o[d][v] * f0 + ob[(16 * d + v) * TPG + tid] * f1;
+        }
+    }
+
+    // ---- epilogue: the two lanes of a row hold disjoint keys; a lane holds dims
+    // 32 d + 8 j + 4 eta + {0..3}
+    const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+    if (!row_ok) return;
+    if (nsplit == 1) {
+        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // (every score minus infinity: zeros)
+        bf16_t* out = reinterpret_cast<bf16_t*>(a.out) + orow * DH;
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                bf16x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = (__bf16)(o[d][4 * j + e] * inv);
+                *reinterpret_cast<bf16x4*>(out + 32 * d + 8 * j + 4 * eta) = w;
+            }
+        if (a.lse && eta == 0) a.lse[orow] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
+        return;
+    }
+    const size_t nrow = (size_t)total_rows * a.Hkv;          // (b R Hq)
+    float* po = a.part + ((size_t)split * nrow + orow) * DH;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<float4*>(po + 32 * d + 8 * j + 4 * eta) =
+                make_float4(o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]);
+    if (eta == 0)
+        *reinterpret_cast<float2*>(a.part + (size_t)nsplit * nrow * DH + ((size_t)split * nrow + orow) * 2) = make_float2(m_run, l_tot);
+}
+
+// Merge of key splits: out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) in
+// split order.  A thread per (row, head, 4 dims).
+template <int DH, typename T>
+__global__ __launch_bounds__(256) void shared_attn_combine_kernel(const float* __restrict__ part, int ns, size_t nrow,
+                                                                  T* __restrict__ out, float* __restrict__ lse) {
+    const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x, row = t / (DH / 4);
+    const int q4 = t % (DH / 4);
+    if (row >= nrow) return;
+    const float2* ml = reinterpret_cast<const float2*>(part + (size_t)ns * nrow * DH);
+    float M = kLeast;
+    for (int s = 0; s < ns; ++s) M = fmaxf(M, ml[s * nrow + row].x);
+    float l = 0.f;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < ns; ++s) {
+        const float2 v = ml[s * nrow + row];
+        const float f = __builtin_amdgcn_exp2f(v.x - M);
+        l += v.y * f;
+        acc += reinterpret_cast<const floatx4*>(part + (s * nrow + row) * DH)[q4] * f;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if constexpr (sizeof(T) == 2) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (__bf16)(acc[e] * inv);
+        *reinterpret_cast<bf16x4*>(out + row * DH + 4 * q4) = w;
+    } else {
+        st_f4(out + row * DH + 4 * q4, acc * inv);
+    }
+    if (lse && q4 == 0) lse[row] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+}
+
+// fp32, on v_mfma_f32_16x16x4_f32: a workgroup takes 16 rows of the same row
+// space; its four waves take interleaved tiles of 32 keys, shared ones first, and
+// merge through LDS in wave order.  S^T = K Q^T leaves lane l (token l % 16, g = l / 16)
+// with keys 4g .. 4g + 3, and the B operand of step e of O^T += V^T P^T is key
+// 4g + e, so probabilities are used where they are.
+constexpr int kWavesF = 4, kKeysF = 32;
+
+template <int DH>
+__global__ __launch_bounds__(64 * kWavesF) void shared_attn_f32_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
+    constexpr int NC = DH / 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lr = lane & 15, g = lane >> 4;
+    int bid = blockIdx.x;
+    {
+        const int total = gridDim.x, per = total >> 3, more = total & 7, x = bid & 7;
+        bid = x * per + min(x, more) + (bid >> 3);
+    }
+    const int rt = bid % rowtiles, split = bid / rowtiles % nsplit, kvh = bid / rowtiles / nsplit;
+    const int GQ = a.Hq / a.Hkv, R = 2 * a.B, RS = GQ * R, total_rows = a.b * RS;
+    const int s0 = rt * 16 / RS, nseq = (min(rt * 16 + 16, total_rows) - 1) / RS - s0 + 1;   // at most 8
+    const int nsh = (a.Ps + kKeysF - 1) / kKeysF;
+    int plen = 0, upto = 0;
+    if (lane < nseq) {
+        plen = a.prefix ? min(max(a.prefix[s0 + lane], 0), a.P) : a.P;
+        upto = (plen + R + kKeysF - 1) / kKeysF;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int below = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += below;
+    }
+    const int ntiles = nsh + __builtin_amdgcn_readlane(upto, 63);
+    const int t_begin = (int)((long long)ntiles * split / nsplit), t_end = (int)((long long)ntiles * (split + 1) / nsplit);
+
+    const int rho = rt * 16 + lr, rc = min(rho, total_rows - 1);
+    const int seq = rc / RS, r = rc % RS / GQ, h = kvh * GQ + rc % GQ;
+    const size_t orow = ((size_t)seq * R + r) * a.Hq + h;
+    floatx4 qf[NC], o[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        qf[c] = ld_f4(reinterpret_cast<const float*>(a.q) + orow * DH + 16 * c + 4 * g);
+        o[c] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int i = r % a.B;
+    const bool shadow = r >= a.B;
+    const uint8_t* st = a.state + (size_t)seq * a.B;
+    const float* cf = a.conf + (size_t)seq * a.B;
+    const int si = st[i];
+    const float ci = cf[i], sl2 = a.scale * kLog2e;
+    float m = kLeast, l = 0.f;
+    for (int t = t_begin + wave; t < t_end; t += kWavesF) {
+        int k0, nk, tseq = -1, p = 0;
+        if (t < nsh) {
+            k0 = t * kKeysF;
+            nk = a.Ps;
+        } else {
+            const int u = t - nsh, q = __builtin_popcountll(__ballot(upto <= u));
+            tseq = s0 + q;
+            p = __builtin_amdgcn_readlane(plen, q);
+            k0 = (u - (q ? __builtin_amdgcn_readlane(upto, q - 1) : 0)) * kKeysF;
+            nk = p + R;
+        }
+        const size_t head = tseq < 0 ? (size_t)kvh : (size_t)tseq * a.Hkv + kvh;
+        const int vcap = tseq < 0 ? a.cap_sh : a.cap;
+        const float* kk = reinterpret_cast<const float*>(tseq < 0 ? a.ksh : a.k) + head * vcap * DH;
+        const float* vv = reinterpret_cast<const float*>(tseq < 0 ? a.vsh : a.v) + head * vcap * DH;
+        floatx4 sc[2], vf[2][NC];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float* kr = kk + (size_t)min(k0 + 16 * b + lr, nk - 1) * DH + 4 * g;
+            floatx4 kf[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kf[c] = ld_f4(kr + 16 * c);
+            const int kv = k0 + 16 * b + 4 * g;              // (keys past the last one read as zero)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const float* vr = vv + (size_t)(16 * c + lr) * vcap + kv;
+                if (kv + 4 <= nk) {
+                    vf[b][c] = ld_f4(vr);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vf[b][c][e] = kv + e < nk ? vr[e] : 0.f;
+                }
+            }
+            sc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[b] = mfma16x16x4f(kf[c][e], qf[c][e], sc[b]);
+        }
+        float mt = m;
+        uint32_t vis = 0;                                    // bit 4b + e: the row sees key k0 + 16b + 4g + e
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = k0 + 16 * b + 4 * g + e;
+                bool see = key < nk && (tseq < 0 || tseq == seq);
+                if (see && tseq >= 0 && key >= p) {
+                    const int j = key - p, jj = j < a.B ? j : j - a.B;
+                    see = take_x(si, st[jj], ci, cf[jj], i, jj, shadow, a.flags) == (j < a.B);
+                }
+                sc[b][e] *= sl2;
+                if (see) { vis |= 1u << (4 * b + e); mt = fmaxf(mt, sc[b][e]); }
+            }
+        mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
+        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+        const float alpha = __builtin_amdgcn_exp2f(m - mt);
+        float ps = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float pe = (vis >> (4 * b + e)) & 1u ? __builtin_amdgcn_exp2f(sc[b][e] - mt) : 0.f;
+                sc[b][e] = pe;
+                ps += pe;
+            }
+        l = l * alpha + ps;
+        m = mt;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[c] *= alpha;
+        // a key that a row does not see adds nothing to it, whatever V holds there
+        bool odd = false;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd |= !(fabsf(vf[b][c][e]) < INFINITY);
+        if (!__any(odd)) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[c] = mfma16x16x4f(vf[b][c][e], sc[b][e], o[c]);
+        } else {
+            for (int key = 0; key < kKeysF; ++key) {
+                const int b = key >> 4, gk = (key >> 2) & 3, e = key & 3;
+                float pe = 0.f;
+#pragma unroll
+                for (int b2 = 0; b2 < 2; ++b2)
+#pragma unroll
+                    for (int e2 = 0; e2 < 4; ++e2)
+                        if (b2 == b && e2 == e) pe = sc[b2][e2];
+                pe = __shfl(pe, lr + 16 * gk, 64);
+                const uint32_t w = __shfl((int)vis, lr + 16 * gk, 64);
+                if (!((w >> (4 * b + e)) & 1u)) continue;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                        o[c][d] += pe * vv[(size_t)(16 * c + 4 * g + d) * vcap + k0 + key];
+            }
+        }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    __shared__ floatx4 po[kWavesF][NC][64];
+    __shared__ float pm[kWavesF][16], pl[kWavesF][16];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) po[wave][c][lane] = o[c];
+    if (g == 0) { pm[wave][lr] = m; pl[wave][lr] = l; }
+    __syncthreads();
+    float M = pm[0][lr];
+#pragma unroll
+    for (int w = 1; w < kWavesF; ++w) M = fmaxf(M, pm[w][lr]);
+    float f[kWavesF], lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWavesF; ++w) {
+        f[w] = __builtin_amdgcn_exp2f(pm[w][lr] - M);
+        lt += pl[w][lr] * f[w];
+    }
+    if (rho >= total_rows) return;
+    const size_t nrow = (size_t)total_rows * a.Hkv;
+    const float inv = nsplit > 1 ? 1.f : (lt == 0.f ? 0.f : 1.f / lt);
+    float* dst = nsplit > 1 ? a.part + ((size_t)split * nrow + orow) * DH : reinterpret_cast<float*>(a.out) + orow * DH;
+    for (int c = wave; c < NC; c += kWavesF) {
+        floatx4 v = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWavesF; ++w) v += po[w][c][lane] * f[w];
+        st_f4(dst + 16 * c + 4 * g, v * inv);
+    }
+    if (wave == 0 && g == 0) {
+        if (nsplit > 1)
+            *reinterpret_cast<float2*>(a.part + (size_t)nsplit * nrow * DH + ((size_t)split * nrow + orow) * 2) = make_float2(M, lt);
+        else if (a.lse)
+            a.lse[orow] = lt == 0.f ? -INFINITY : (M + __log2f(lt)) * kLn2;
+    }
+}
+
+struct SharedCfg {
+    int waves, g, rowtiles, ns;
+};
+
+SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
+    SharedCfg c{};
+    const long rows = (long)b * 2 * B * (Hq / Hkv);
+    if (dtype == DARD_DTYPE_F32) {
+        c.waves = kWavesF;
+        c.g = 1;
+        c.rowtiles = (int)((rows + 15) / 16);
+        const long wgs = (long)c.rowtiles * Hkv, tiles = ((long)Ps + P + 2 * B) / kKeysF + 1;
+        c.ns = (int)std::max<long>(1, std::min<long>(std::min<long>(512 / wgs, tiles / (2 * kWavesF)), kMaxSplit));
+        return c;
+    }
+    c.waves = rows > 64 ? 4 : 2;
+    c.rowtiles = (int)((rows + 32 * c.waves - 1) / (32 * c.waves));
+    const long wgs = (long)c.rowtiles * Hkv;
+    const long RS = 2L * B * (Hq / Hkv), seqs = std::min<long>(b, (32 * c.waves + RS - 1) / RS);
+    const long tiles = ((long)Ps + kKeys - 1) / kKeys + seqs * (((long)P + 2 * B + kKeys - 1) / kKeys);
+    c.g = 1;
+    c.ns = (int)std::max<long>(1, std::min<long>(std::min<long>(512 / wgs, tiles / 4), kMaxSplit));
+    return c;
+}
+
+}  // namespace
+
+size_t shared_attention_partial_floats(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P) {
+    const SharedCfg c = shared_cfg(dtype, b, B, Hq, Hkv, Ps, P);
+    return c.ns <= 1 ? 0 : (size_t)c.ns * b * 2 * B * Hq * (dh + 2);
+}
+
+template <int DH>
+static hipError_t launch_shared(int dtype, const SharedAttnArgs& a, hipStream_t s) {
+    const SharedCfg c = shared_cfg(dtype, a.b, a.B, a.Hq, a.Hkv, a.Ps, a.P);
+    const dim3 grid((unsigned)((long)c.rowtiles * a.Hkv * c.ns));
+    const bool f32 = dtype == DARD_DTYPE_F32;
+    if (f32) {
+        launch(shared_attn_f32_kernel<DH>, grid, dim3(64 * kWavesF), 0, s, a, c.rowtiles, c.ns);
+    } else {
+        const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8;
+        auto k = c.waves == 4 ? (kv8 ? shared_attn_kernel<DH, 4, 1, true> : shared_attn_kernel<DH, 4, 1, false>)
+                              : (kv8 ? shared_attn_kernel<DH, 2, 1, true> : shared_attn_kernel<DH, 2, 1, false>);
+        launch(k, grid, dim3(64 * c.waves), 0, s, a, c.rowtiles, c.ns);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || c.ns == 1) return e;
+    const size_t nrow = (size_t)a.b * 2 * a.B * a.Hq;
+    const dim3 cg((unsigned)((nrow * (DH / 4) + 255) / 256));
+    if (f32)
+        launch(shared_attn_combine_kernel<DH, float>, cg, dim3(256), 0, s, (const float*)a.part, c.ns, nrow, (float*)a.out, a.lse);
+    else
+        launch(shared_attn_combine_kernel<DH, bf16_t>, cg, dim3(256), 0, s, (const float*)a.part, c.ns, nrow, (bf16_t*)a.out, a.lse);
+    return hipGetLastError();
+}
+
+hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, hipStream_t s) {
+    return a.dh == 128 ? launch_shared<128>(dtype, a, s) : launch_shared<64>(dtype, a, s);
+}
+
+}  // namespace dard

@@ -40,6 +40,8 @@ EXPORTS = [
     "dard_quantize_mx", "dard_dequantize_mx", "dard_resid_norm_mx", "dard_packed_mx_bytes", "dard_pack_matrix_mx",
     "dard_linear_mx_workspace_bytes", "dard_linear_mx", "dard_linear_mx_plan", "dard_kv_write_mx", "dard_kv_read_mx",
     "dard_attention_mx_workspace_bytes", "dard_masked_attention_mx",
+    "dard_attention_shared_workspace_bytes", "dard_masked_attention_shared", "dard_key_weights_workspace_bytes",
+    "dard_key_weights", "dard_kv_select_workspace_bytes", "dard_kv_select", "dard_kv_compact",
     "dard_trace_enable",
     "dard_trace_read", "dard_trace_reset", "dard_trace_sample",
 ]
@@ -120,6 +122,15 @@ def lib():
             "dard_attention_mx_workspace_bytes": (sz, [i32, i32, i32, i32, i32, i32]),
             "dard_masked_attention_mx": (i32, [vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, i32, i32, i32, f32,
                                                u32, vp, vp, sz, vp]),
+            "dard_attention_shared_workspace_bytes": (sz, [i32] * 8),
+            "dard_masked_attention_shared": (i32, [i32, vp, vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, vp, i32, i32, i32,
+                                                   i32, i32, f32, u32, vp, vp, vp, sz, vp]),
+            "dard_key_weights_workspace_bytes": (sz, [i32] * 7),
+            "dard_key_weights": (i32, [i32, vp, vp, vp, i32, vp, i32, i32, i32, i32, i32, i32, f32, f32, vp, i64, vp, sz,
+                                       vp]),
+            "dard_kv_select_workspace_bytes": (sz, [i32] * 4),
+            "dard_kv_select": (i32, [vp, i64, i32, vp, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]),
+            "dard_kv_compact": (i32, [i32, vp, vp, i32, vp, i64, vp, i32, vp, i32, vp, i32, i32, i32, vp]),
             "dard_trace_enable": (i32, [u32]),
             "dard_trace_read": (i32, [i32, ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_double)]),
             "dard_trace_reset": (i32, []),
@@ -487,6 +498,126 @@ def dard_masked_attention_mx(q, cache, P, state, conf, scale, flags, out, ws=Non
     (qp, kc, ks, vc, vs, pre, sp, cp, op, room), st = _args(stream, (q, *cache, _mx_prefix(prefix, b), state, conf, out, ws))
     _check(lib().dard_masked_attention_mx(qp, kc, ks, vc, vs, P, pre, cap, sp, cp, b, R // 2, Hq, Hkv, dh, scale, flags,
                                           op, room, _nbytes(ws), st))
+
+
+def _kv_dt(q, *caches):
+    """Operation type of q (or None) and the caches; FP8 caches hold E4M3 codes as uint8 or float8_e4m3fn."""
+    kt = caches[0].dtype
+    for t in caches:
+        if t is not None and t.dtype is not kt:
+            raise ValueError(f"the caches must have one type, got {kt} and {t.dtype}")
+    if kt is torch.uint8 or kt is torch.float8_e4m3fn:
+        want, dt = torch.bfloat16, DTYPE_BF16_KV_FP8
+    elif kt is torch.bfloat16 or kt is torch.float32:
+        want, dt = kt, DTYPE_BF16 if kt is torch.bfloat16 else DTYPE_F32
+    else:
+        raise ValueError(f"a cache must be bfloat16, float32 or FP8 codes, got {kt}")
+    if q is not None and q.dtype is not want:
+        raise ValueError(f"q must be {want} for a cache of {kt}, got {q.dtype}")
+    return dt
+
+
+def _lengths(t, b, what):
+    if t is not None and (t.dtype is not torch.int32 or t.numel() != b):
+        raise ValueError(f"{what} must be int32 [{b}]")
+    return t
+
+
+def _sums_ld(w, b, Hkv, P):
+    """Elements between the rows of weights [b][Hkv][>= P] (float32, evenly spaced rows)."""
+    if w.dtype is not torch.float32 or w.dim() != 3 or w.shape[0] != b or w.shape[1] != Hkv or w.shape[2] < P:
+        raise ValueError(f"weights must be float32 [{b}][{Hkv}][>= {P}], got {w.dtype} {tuple(w.shape)}")
+    sb, sh, sk = w.stride()
+    ld = sh if Hkv > 1 else (sb if b > 1 else max(w.shape[2], 1))
+    if (w.shape[2] > 1 and sk != 1) or (b > 1 and sb != Hkv * ld) or ld < P:
+        raise ValueError("weights must have contiguous, evenly spaced rows")
+    return ld
+
+
+def dard_attention_shared_workspace_bytes(dtype, b, B, Hq, Hkv, dh, Ps, P):
+    return lib().dard_attention_shared_workspace_bytes(dtype, b, B, Hq, Hkv, dh, Ps, P)
+
+
+def dard_masked_attention_shared(q, k_shared, v_shared, Ps, k, v, P, state, conf, scale, flags, out, lse=None, ws=None,
+                                 prefix=None, stream=None):
+    """dard_masked_attention of a batch with Ps keys of a shared cache (k_shared [Hkv][cap_shared][dh], v_shared
+    [Hkv][dh][cap_shared]; None where Ps is 0) before each sequence's own (k [b][Hkv][cap][dh], v [b][Hkv][dh][cap]:
+    prefix[s] or P keys, then the block); lse: float32 [b][2B][Hq] or None."""
+    b, R, Hq, dh = q.shape
+    _, Hkv, cap, _ = k.shape
+    if k.shape != (b, Hkv, cap, dh) or v.shape != (b, Hkv, dh, cap):
+        raise ValueError(f"k must be [b][Hkv][cap][dh], v [b][Hkv][dh][cap], got {tuple(k.shape)} and {tuple(v.shape)}")
+    cap_sh = 0
+    if k_shared is not None or v_shared is not None:
+        if k_shared is None or v_shared is None:
+            raise ValueError("k_shared and v_shared go together")
+        cap_sh = k_shared.shape[1]
+        if k_shared.shape != (Hkv, cap_sh, dh) or v_shared.shape != (Hkv, dh, cap_sh):
+            raise ValueError("k_shared must be [Hkv][cap_shared][dh], v_shared [Hkv][dh][cap_shared]")
+    if out.shape != q.shape or out.dtype is not q.dtype:
+        raise ValueError("out must be as q")
+    if R % 2 or state.shape != (b, R // 2) or conf.shape != state.shape:
+        raise ValueError(f"state and conf must be [b][B] = {(b, R // 2)}")
+    if state.dtype is not torch.uint8 or conf.dtype is not torch.float32:
+        raise ValueError("state must be uint8, conf float32")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (b, R, Hq)):
+        raise ValueError(f"lse must be float32 {(b, R, Hq)}")
+    dt = _kv_dt(q, k, v, k_shared, v_shared)
+    (qp, ks, vs, kp, vp, pre, sp, cp, op, lp, room), st = _args(
+        stream, (q, k_shared, v_shared, k, v, _lengths(prefix, b, "prefix"), state, conf, out, lse, ws))
+    _check(lib().dard_masked_attention_shared(dt, qp, ks, vs, Ps, cap_sh, kp, vp, P, pre, cap, sp, cp, b, R // 2, Hq, Hkv,
+                                              dh, scale, flags, op, lp, room, _nbytes(ws), st))
+
+
+def dard_key_weights_workspace_bytes(dtype, b, R, Hq, Hkv, dh, P):
+    return lib().dard_key_weights_workspace_bytes(dtype, b, R, Hq, Hkv, dh, P)
+
+
+def dard_key_weights(q, lse, k, P, scale, decay, weights, ws=None, prefix=None, stream=None):
+    """weights [b][Hkv][>= P] (float32, rows may be further apart) = decay weights + the softmax weight of every prefix
+    key of k [b][Hkv][cap][dh], summed over the rows q [b][R][Hq][dh] with lse [b][R][Hq]."""
+    b, R, Hq, dh = q.shape
+    _, Hkv, cap, _ = k.shape
+    if k.shape != (b, Hkv, cap, dh):
+        raise ValueError(f"k must be [b][Hkv][cap][dh], got {tuple(k.shape)}")
+    if lse.dtype is not torch.float32 or lse.shape != (b, R, Hq):
+        raise ValueError(f"lse must be float32 {(b, R, Hq)}")
+    ld = _sums_ld(weights, b, Hkv, P)
+    dt = _kv_dt(q, k)
+    (qp, lp, kp, pre, room, wp), st = _args(stream, (q, lse, k, _lengths(prefix, b, "prefix"), ws), (weights,))
+    _check(lib().dard_key_weights(dt, qp, lp, kp, P, pre, cap, b, R, Hq, Hkv, dh, scale, decay, wp, ld, room, _nbytes(ws),
+                                  st))
+
+
+def dard_kv_select_workspace_bytes(b, Hkv, P, n):
+    return lib().dard_kv_select_workspace_bytes(b, Hkv, P, n)
+
+
+def dard_kv_select(weights, P, keep, first=0, last=0, kept=None, ws=None, prefix=None, stream=None):
+    """keep [b][Hkv][n] (int32): ascending indices of the keys of the largest weights [b][Hkv][>= P], the first and the
+    last few always among them, -1 from kept[s] = min(n, prefix[s] or P) on; kept: int32 [b] or None."""
+    if keep.dtype is not torch.int32 or keep.dim() != 3:
+        raise ValueError("keep must be int32 [b][Hkv][n]")
+    b, Hkv, n = keep.shape
+    ld = _sums_ld(weights, b, Hkv, P)
+    (kp, np_, pre, room, wp), st = _args(
+        stream, (keep, _lengths(kept, b, "kept"), _lengths(prefix, b, "prefix"), ws), (weights,))
+    _check(lib().dard_kv_select(wp, ld, P, pre, b, Hkv, n, first, last, kp, np_, room, _nbytes(ws), st))
+
+
+def dard_kv_compact(k, v, keep, P, weights=None, kept=None, prefix=None, stream=None):
+    """Keys keep[s][g][j] of k [b][Hkv][cap][dh], v [b][Hkv][dh][cap] and weights [b][Hkv][>= P] (or None) to places j <
+    kept[s] (None: keep's n), in place; freed weights become 0."""
+    b, Hkv, cap, dh = k.shape
+    if v.shape != (b, Hkv, dh, cap):
+        raise ValueError(f"v must be [b][Hkv][dh][cap] = {(b, Hkv, dh, cap)}, got {tuple(v.shape)}")
+    if keep.dtype is not torch.int32 or keep.dim() != 3 or keep.shape[:2] != (b, Hkv):
+        raise ValueError(f"keep must be int32 [{b}][{Hkv}][n]")
+    dt = _kv_dt(None, k, v)
+    ld = 0 if weights is None else _sums_ld(weights, b, Hkv, P)
+    (kp, vp, ip, np_, pre, *w), st = _args(stream, (k, v, keep, _lengths(kept, b, "kept"), _lengths(prefix, b, "prefix")),
+                                           () if weights is None else (weights,))
+    _check(lib().dard_kv_compact(dt, kp, vp, cap, w[0] if w else None, ld, ip, keep.shape[2], np_, P, pre, b, Hkv, dh, st))
 
 
 def dard_trace_enable(mask):
