@@ -664,6 +664,7 @@ int check_key_weights(int dtype, int b, int R, int Hq, int Hkv, int dh, int P) {
     if (int rc = check_heads(b, Hq, Hkv, dh)) return rc;
     if (R < 1 || P < 0) return fail(DARD_ERR_SHAPE, "need R >= 1 and P >= 0");
     if ((double)R * Hq > 1073741824.0) return fail(DARD_ERR_SHAPE, "R * Hq must be at most 2^30");
+    if (Hq / Hkv > 32768) return fail(DARD_ERR_SHAPE, "Hq / Hkv must be at most 32768");
     if ((double)b * Hkv * (P / 128 + 1.0) >= 8388608.0) return fail(DARD_ERR_SHAPE, "too many keys in one call");
     return DARD_OK;
 }

@@ -34,14 +34,16 @@ constexpr int kWRows = 64;       // rows of a stage
 
 // A workgroup's (sequence, KV head), key tile and row split: splits fastest, then
 // key tiles, dealt to the XCDs in contiguous runs, so those that read the same rows
-// share an L2.
+// share an L2; heads go to the runs in turn where they divide by 8, so that every
+// XCD has heads of every sequence, however their lengths differ.
 struct WeightUnit {
     int head, kt, split;
 };
 __device__ __forceinline__ WeightUnit weight_unit(const KeyWeightArgs& a, int nsplit, int tile) {
-    const int total = gridDim.x, x = blockIdx.x & 7, ktiles = (a.P + tile - 1) / tile;
+    const int total = gridDim.x, x = blockIdx.x & 7, ktiles = (a.P + tile - 1) / tile, heads = a.b * a.Hkv;
     const int bid = x * (total >> 3) + min(x, total & 7) + (blockIdx.x >> 3);
-    return {bid / nsplit / ktiles, bid / nsplit % ktiles, bid % nsplit};
+    const int slot = bid / nsplit / ktiles, per = heads >> 3;
+    return {heads & 7 ? slot : slot % per * 8 + slot / per, bid / nsplit % ktiles, bid % nsplit};
 }
 
 // decay = 0 does not read the old sum (it may hold anything).
@@ -50,10 +52,32 @@ __device__ __forceinline__ void add_weight(const KeyWeightArgs& a, int head, int
     *w = a.decay == 0.f ? x : fmaf(a.decay, *w, x);
 }
 
+// Sums of 16 values over the 32 lanes of a half wave: each exchange halves the
+// values that a lane carries, so 16 shuffles do what 80 would.  Lanes 2v and 2v + 1
+// return value v.
+__device__ __forceinline__ float half_sums(const float (&x)[16], int lr) {
+    float y[8];
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+        const bool up = lr & 16;
+        y[v] = (up ? x[v + 8] : x[v]) + __shfl_xor(up ? x[v] : x[v + 8], 16, 64);
+    }
+#pragma unroll
+    for (int o = 8, n = 4; n >= 1; o >>= 1, n >>= 1) {
+        const bool up = lr & o;
+#pragma unroll
+        for (int v = 0; v < n; ++v) {
+            const float give = up ? y[v] : y[v + n], have = up ? y[v + n] : y[v];
+            y[v] = have + __shfl_xor(give, o, 64);
+        }
+    }
+    return y[0] + __shfl_xor(y[0], 1, 64);
+}
+
 template <int DH, int KB, bool KV8>
 __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int nsplit) {
     constexpr int NC = DH / 16, CH = DH / 8;                 // MFMA steps; 16-byte chunks of a row
-    constexpr int STAGE = kWRows * DH * 2, NI = kWRows * CH / 256;
+    constexpr int STAGE = kWRows * DH * 2, NI = kWRows * CH / 256, HALVES = kWRows / 32;
     __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef __attribute__((address_space(1))) void* glb_ptr;
@@ -66,22 +90,6 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
     const int GQ = a.Hq / a.Hkv, rows = GQ * a.R;
     const int ntile = (rows + kWRows - 1) / kWRows;
     const int t0 = (int)((long long)ntile * split / nsplit), t1 = (int)((long long)ntile * (split + 1) / nsplit);
-
-    // rows in the order (position row, head): GQ neighbours in memory
-    const bf16_t* qb = reinterpret_cast<const bf16_t*>(a.q) + ((size_t)s * a.R * a.Hq + (size_t)g * GQ) * DH;
-    const float* lb = a.lse + (size_t)s * a.R * a.Hq + (size_t)g * GQ;
-    auto row_at = [&](int rho) __attribute__((always_inline)) { return (size_t)(rho / GQ) * a.Hq + rho % GQ; };
-    // chunk c of row r sits in slot c ^ swizzle(r): the operand reads of 16 lanes hit different banks
-    auto swz = [&](int r) __attribute__((always_inline)) { return CH == 16 ? r & 15 : (r ^ (r >> 3)) & 7; };
-    auto issue = [&](int t, char* dst) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const int q = (wave * NI + j) * 64 + lane, r = q / CH, c = (q % CH) ^ swz(r);
-            const bf16_t* src = qb + row_at(min(t * kWRows + r, rows - 1)) * DH + 8 * c;
-            __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
-        }
-    };
-    if (t0 < t1) issue(t0, smem);
 
     // this wave's keys: A operand row lr of block kb; a key past the last one repeats it.
     // Step c of an operand takes chunk ch(c, eta) of its row (any order will do that K and
@@ -104,6 +112,39 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
             for (int c = 0; c < NC; ++c) kf[kb][c] = ld_bf16x8(reinterpret_cast<const bf16_t*>(a.k) + row + 8 * ch(c));
         }
     }
+
+    // rows in the order (position row, head): GQ neighbours in memory.  A stage's first
+    // row is divided once, a row of it by multiplication (rem + i < GQ + 64, GQ <= 32768)
+    const bf16_t* qb = reinterpret_cast<const bf16_t*>(a.q) + ((size_t)s * a.R * a.Hq + (size_t)g * GQ) * DH;
+    const float* lb = a.lse + (size_t)s * a.R * a.Hq + (size_t)g * GQ;
+    const uint32_t magic = GQ > 1 ? 0xFFFFFFFFu / (uint32_t)GQ + 1u : 0u;
+    auto row_at = [&](int pos, int rem, int i) __attribute__((always_inline)) {
+        const uint32_t x = rem + i, d = GQ > 1 ? __umulhi(x, magic) : x;
+        return (size_t)(pos + (int)d) * a.Hq + (x - d * GQ);
+    };
+    // chunk c of row r sits in slot c ^ swizzle(r): the operand reads of 16 lanes hit different banks
+    auto swz = [&](int r) __attribute__((always_inline)) { return CH == 16 ? r & 15 : (r ^ (r >> 3)) & 7; };
+    float L[HALVES];
+    auto issue = [&](int t, char* dst) __attribute__((always_inline)) {
+        const int pos = t * kWRows / GQ, rem = t * kWRows % GQ, most = rows - 1 - t * kWRows;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int q = (wave * NI + j) * 64 + lane, r = q / CH, c = (q % CH) ^ swz(r);
+            const bf16_t* src = qb + row_at(pos, rem, min(r, most)) * DH + 8 * c;
+            __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+        }
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) L[h] = lb[row_at(pos, rem, min(32 * h + lr, most))];
+    };
+    if (t0 < t1) issue(t0, smem);
+    // the old sums that this lane will add to (lanes 2v of a half: value v of each block)
+    const int mykey = 8 * (lr >> 3) + 4 * eta + ((lr >> 1) & 3);
+    float old[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        const int key = k0 + 32 * kb + mykey;
+        old[kb] = a.decay != 0.f && nsplit == 1 && key < p ? a.weights[(size_t)un.head * a.ldw + key] : 0.f;
+    }
     const float sl2 = a.scale * kLog2e;
     float acc[KB][16];
 #pragma unroll
@@ -115,19 +156,22 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
         char* cur = smem + ((t - t0) & 1) * STAGE;
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();                                     // stage t has arrived, and stage t - 1 is read
+        float bias[HALVES];
+        bool live[HALVES];
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {                   // (a row without a sum counts nothing; NaN stays NaN)
+            live[h] = t * kWRows + 32 * h + lr < rows && (fabsf(L[h]) < INFINITY || L[h] != L[h]);
+            bias[h] = -L[h] * kLog2e;
+        }
         if (t + 1 < t1) issue(t + 1, smem + ((t + 1 - t0) & 1) * STAGE);
 #pragma unroll
-        for (int half = 0; half < kWRows / 32; ++half) {
-            const int rho = t * kWRows + 32 * half + lr;
-            const float L = rho < rows ? lb[row_at(rho)] : INFINITY;
-            const bool live = fabsf(L) < INFINITY || L != L; // (a row without a sum counts nothing; NaN stays NaN)
-            const float bias = -L * kLog2e;
+        for (int half = 0; half < HALVES; ++half) {
             bf16x8 qf[NC];
             const int r = 32 * half + lr;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 qf[c] = *reinterpret_cast<const bf16x8*>(cur + 16 * (r * CH + (ch(c) ^ swz(r))));
-            const bool all = __all(live);
+            const bool all = __all(live[half]);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 floatx16 sc;
@@ -137,29 +181,25 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
                 for (int c = 0; c < NC; ++c) sc = mfma32x32x16(kf[kb][c], qf[c], sc);
                 if (all) {
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[kb][v] += __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias));
+                    for (int v = 0; v < 16; ++v) acc[kb][v] += __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias[half]));
                 } else {
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
-                        acc[kb][v] += live ? __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias)) : 0.f;
+                        acc[kb][v] += live[half] ? __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias[half])) : 0.f;
                 }
             }
         }
     }
-    // sum over the 32 lanes of a half: element v of block kb is key 32 kb + 8 (v / 4) + 4 eta + v % 4
+    // element v of block kb is key 32 kb + 8 (v / 4) + 4 eta + v % 4
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            float x = acc[kb][v];
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-            const int key = k0 + 32 * kb + 8 * (v >> 2) + 4 * eta + (v & 3);
-            if (lr == v && key < p) {
-                if (nsplit > 1) a.part[((size_t)split * a.b * a.Hkv + un.head) * a.P + key] = x;
-                else add_weight(a, un.head, key, x);
-            }
+    for (int kb = 0; kb < KB; ++kb) {
+        const float x = half_sums(acc[kb], lr);
+        const int key = k0 + 32 * kb + mykey;
+        if ((lr & 1) == 0 && key < p) {
+            if (nsplit > 1) a.part[((size_t)split * a.b * a.Hkv + un.head) * a.P + key] = x;
+            else a.weights[(size_t)un.head * a.ldw + key] = fmaf(a.decay, old[kb], x);
         }
+    }
 }
 
 // The same on v_mfma_f32_16x16x4_f32: a wave takes 32 keys, rows come straight from memory.
@@ -237,7 +277,7 @@ struct WeightCfg {
 WeightCfg weight_cfg(int dtype, int b, int R, int Hq, int Hkv, int P) {
     WeightCfg c{};
     const long rows = (long)R * (Hq / Hkv), heads = (long)b * Hkv;
-    c.kb = dtype == DARD_DTYPE_F32 || heads * ((P + 255) / 256) < 512 ? 1 : 2;
+    c.kb = dtype == DARD_DTYPE_F32 || rows < 512 || heads * ((P + 255) / 256) < 256 ? 1 : 2;
     c.ktiles = (P + 128 * c.kb - 1) / (128 * c.kb);
     const long wgs = heads * c.ktiles, tiles = (rows + kWRows - 1) / kWRows;
     c.ns = (int)std::max<long>(1, std::min<long>(512 / wgs, tiles / 4));
@@ -260,8 +300,15 @@ __device__ __forceinline__ uint32_t sum_rank(float w) {
     return (u >> 31) ? ~u : u | 0x80000000u;                 // -inf: 0x007FFFFF; +inf: 0xFF800000
 }
 
+// HELD: the row's sums fit the registers (kHeld keys a thread) and are read once;
+// else every pass reads them again, 16 keys a thread in flight.
+constexpr int kHeld = 8;
+
+template <bool HELD>
 __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) {
-    __shared__ uint32_t hist[2048];
+    // histogram copies by lane: equal sums in neighbouring lanes would queue at one counter
+    constexpr int COPIES = 4;
+    __shared__ uint32_t hist[COPIES][2048];
     __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
     __shared__ uint32_t found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -275,8 +322,46 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
         for (int i = tid; i < m; i += kSelThreads) keep[i] = i;
         return;
     }
-    auto rank = [&](int j) __attribute__((always_inline)) {
-        return j < a.first || j >= p - a.last ? 0xFFFFFFFFu : sum_rank(w[j]);
+    // a wave's keys: a run of whole 256s, four neighbours a lane
+    const int per = ((p + kSelWaves - 1) / kSelWaves + 255) / 256 * 256, j0 = wave * per, j1 = min(p, j0 + per);
+    auto fetch = [&](int j) __attribute__((always_inline)) {
+        floatx4 x = {0.f, 0.f, 0.f, 0.f};
+        if (j + 4 <= p) x = ld_f4(w + j);
+        else if (j < p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = w[min(j + e, p - 1)];
+        return x;
+    };
+    auto rank = [&](float x, int j) __attribute__((always_inline)) {
+        return j < a.first || j >= p - a.last ? 0xFFFFFFFFu : sum_rank(x);
+    };
+    floatx4 held[kHeld / 4];
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < kHeld / 4; ++i) held[i] = fetch(j0 + 256 * i + 4 * lane);
+    }
+    // f(ranks of four keys, index of the first) over the wave's run, in order
+    auto run = [&](auto f) __attribute__((always_inline)) {
+        auto four = [&](floatx4 x, int j) __attribute__((always_inline)) {
+            uint32_t u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = rank(x[e], j + e);
+            f(u, j);
+        };
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < kHeld / 4; ++i)
+                if (j0 + 256 * i < j1) four(held[i], j0 + 256 * i + 4 * lane);
+        } else {
+            for (int j = j0; j < j1; j += 1024) {
+                floatx4 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = fetch(j + 256 * i + 4 * lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (j + 256 * i < j1) four(x[i], j + 256 * i + 4 * lane);
+            }
+        }
     };
     // threshold T: fewer than m keys rank above it, m or more at or above it
     uint32_t T = 0, mask = 0;
@@ -284,25 +369,34 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
     constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
 #pragma unroll
     for (int d = 0; d < 3; ++d) {
-        for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
+#pragma unroll
+        for (int i = 0; i < COPIES * 2048 / kSelThreads; ++i) (&hist[0][0])[i * kSelThreads + tid] = 0;
         __syncthreads();
-        for (int j = tid; j < p; j += kSelThreads) {
-            const uint32_t u = rank(j);
-            if ((u & mask) == T) atomicAdd(&hist[(u >> kShift[d]) & ((1u << kBits[d]) - 1)], 1u);
-        }
+        run([&](const uint32_t (&u)[4], int j) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (j + e < j1 && (u[e] & mask) == T)
+                    atomicAdd(&hist[lane % COPIES][(u[e] >> kShift[d]) & ((1u << kBits[d]) - 1)], 1u);
+        });
         __syncthreads();
         // the bin in which the count from the top passes need (integer counts: order plays no part)
-        uint32_t c0 = hist[2047 - 2 * tid], c1 = hist[2046 - 2 * tid];   // this thread's two bins, from the top
-        uint32_t run = c0 + c1;
+        uint32_t c0 = 0, c1 = 0;                             // this thread's two bins, from the top
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            c0 += hist[i][2047 - 2 * tid];
+            c1 += hist[i][2046 - 2 * tid];
+        }
+        uint32_t sum = c0 + c1;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t below = __shfl_up(run, o, 64);
-            if (lane >= o) run += below;
+            const uint32_t below = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += below;
         }
-        if (lane == 63) wsum[wave] = run;
+        if (lane == 63) wsum[wave] = sum;
         __syncthreads();
-        uint32_t before = run - c0 - c1;
-        for (int i = 0; i < wave; ++i) before += wsum[i];
+        uint32_t before = sum - c0 - c1;
+#pragma unroll
+        for (int i = 0; i < kSelWaves; ++i) before += i < wave ? wsum[i] : 0u;
         const uint32_t want = (uint32_t)need;
         if (before < want && before + c0 >= want) { found[0] = 2047 - 2 * tid; found[1] = before; }
         if (before + c0 < want && before + c0 + c1 >= want) { found[0] = 2046 - 2 * tid; found[1] = before + c0; }
@@ -312,30 +406,41 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
         need -= (int)found[1];
     }
     // keys above T, and the first `need` of those that equal it, in index order
-    const int per = ((p + kSelWaves - 1) / kSelWaves + 63) / 64 * 64, j0 = wave * per, j1 = min(p, j0 + per);
     uint32_t above = 0, ties = 0;
-    for (int j = j0; j < j1; j += 64) {
-        const uint32_t u = j + lane < j1 ? rank(j + lane) : 0u;
-        const bool in = j + lane < j1;
-        above += __builtin_popcountll(__ballot(in && u > T));
-        ties += __builtin_popcountll(__ballot(in && u == T));
-    }
+    run([&](const uint32_t (&u)[4], int j) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            above += __builtin_popcountll(__ballot(j + e < j1 && u[e] > T));
+            ties += __builtin_popcountll(__ballot(j + e < j1 && u[e] == T));
+        }
+    });
     if (lane == 0) { wsum[wave] = above; wtie[wave] = ties; }
     __syncthreads();
     uint32_t pos = 0, tie = 0;                               // keys above T, and ties, before this wave's run
-    for (int i = 0; i < wave; ++i) { pos += wsum[i]; tie += wtie[i]; }
-    const uint64_t lower = (1ull << lane) - 1;
-    for (int j = j0; j < j1; j += 64) {
-        const bool in = j + lane < j1;
-        const uint32_t u = in ? rank(j + lane) : 0u;
-        const uint64_t ba = __ballot(in && u > T), bt = __ballot(in && u == T);
-        const uint32_t my_tie = tie + __builtin_popcountll(bt & lower);
-        const bool take = in && (u > T || (u == T && my_tie < (uint32_t)need));
-        const uint32_t at = pos + __builtin_popcountll(ba & lower) + min(my_tie, (uint32_t)need);
-        if (take) keep[at] = j + lane;
-        pos += __builtin_popcountll(ba);
-        tie += __builtin_popcountll(bt);
+#pragma unroll
+    for (int i = 0; i < kSelWaves; ++i) {
+        pos += i < wave ? wsum[i] : 0u;
+        tie += i < wave ? wtie[i] : 0u;
     }
+    const uint64_t lower = (1ull << lane) - 1;
+    run([&](const uint32_t (&u)[4], int j) __attribute__((always_inline)) {
+        uint32_t up = pos, eq = tie;                         // before this lane's four keys
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t ba = __ballot(j + e < j1 && u[e] > T), bt = __ballot(j + e < j1 && u[e] == T);
+            up += __builtin_popcountll(ba & lower);
+            eq += __builtin_popcountll(bt & lower);
+            pos += __builtin_popcountll(ba);
+            tie += __builtin_popcountll(bt);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (j + e >= j1) continue;
+            if (u[e] > T || (u[e] == T && eq < (uint32_t)need)) keep[up + min(eq, (uint32_t)need)] = j + e;
+            up += u[e] > T;
+            eq += u[e] == T;
+        }
+    });
 }
 
 // ---------------------------------------------------------------- compaction
@@ -344,83 +449,126 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
 // then writes that run, which no later chunk reads.  A workgroup owns whole
 // columns (a run of a key's bytes, or rows of the dims-major V), so the order of
 // reads and writes is its own affair.
-constexpr int kMoveThreads = 256;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// K: a workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time.
-template <int SEG>
-__device__ void move_keys(char* k, int row_bytes, const int32_t* keep, int m, int P) {
-    constexpr int LPR = SEG / 16, STEP = kMoveThreads / LPR, U = 8;   // lanes a key, keys a pass, passes in flight
+// A workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time, the
+// next chunk's loads under way while a chunk is written.  (Places past the last one
+// read its source again: loads without branches go out together.)
+template <int THREADS, int SEG, int U = 8>
+__device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t* keep, int m, int P) {
+    constexpr int LPR = SEG / 16, STEP = THREADS / LPR;      // lanes a key, keys a pass (U of them a chunk)
     const int tid = threadIdx.x, key = tid / LPR, at = tid % LPR * 16;
+    if (m < 1) return;
+    u32x4 x[U];
+    int src[U];
+    auto indices = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) src[u] = min(max(keep[min(j0 + u * STEP + key, m - 1)], 0), P - 1);
+    };
+    auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4*>(k + (size_t)src[u] * row_bytes + at);
+    };
+    indices(0);
+    load();
+    indices(U * STEP);
     for (int j0 = 0; j0 < m; j0 += U * STEP) {
-        uint4 x[U];
+        u32x4 y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u] = x[u];
+        // every source of the chunk is in registers; the last chunk's stores, or the first
+        // indices, which are newer, may still be under way
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(U));
+        wg_barrier();
+        if (j0 + U * STEP < m) load();
+        indices(j0 + 2 * U * STEP);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * STEP + key;
-            if (j < m) x[u] = *reinterpret_cast<const uint4*>(k + (size_t)min(max(keep[j], 0), P - 1) * row_bytes + at);
-        }
-        __builtin_amdgcn_s_waitcnt(0);                       // (every source is in registers)
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * STEP + key;
-            if (j < m) *reinterpret_cast<uint4*>(k + (size_t)j * row_bytes + at) = x[u];
+            if (j < m) *reinterpret_cast<u32x4*>(k + (size_t)j * row_bytes + at) = y[u];
         }
     }
 }
 
-// V: a workgroup owns ROWS dims; a thread moves elements of all of them.
-template <typename T, int ROWS>
-__device__ void move_values(T* v, int cap, const int32_t* keep, int m, int P) {
-    constexpr int U = 4;
+// A workgroup owns ROWS rows of `cap` elements; a thread takes the elements of 4
+// bytes of a row at a time: their sources lie close together (the share of keys
+// that is kept apart), so single loads reach whole lines between a wave's lanes.
+template <typename T> struct Word;   // 4 bytes at an element's alignment
+template <> struct Word<float> { typedef uint32_t type; };
+template <> struct Word<uint16_t> { typedef uint32_t type __attribute__((aligned(2))); };
+template <> struct Word<uint8_t> { typedef uint32_t type __attribute__((aligned(1))); };
+
+template <typename T, int THREADS, int ROWS, int E>
+__device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, int m, int P) {
+    constexpr int SU = 4 / sizeof(T), CHUNK = THREADS * SU * E;
     const int tid = threadIdx.x;
-    for (int j0 = 0; j0 < m; j0 += U * kMoveThreads) {
-        T x[U][ROWS];
+    for (int j0 = 0; j0 < m; j0 += CHUNK) {
+        uint32_t x[ROWS][E];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * kMoveThreads + tid;
-            if (j < m) {
-                const int src = min(max(keep[j], 0), P - 1);
+        for (int e = 0; e < E; ++e) {
+            int src[SU];
 #pragma unroll
-                for (int d = 0; d < ROWS; ++d) x[u][d] = v[(size_t)d * cap + src];
+            for (int i = 0; i < SU; ++i) src[i] = min(max(keep[min(j0 + (e * THREADS + tid) * SU + i, m - 1)], 0), P - 1);
+#pragma unroll
+            for (int d = 0; d < ROWS; ++d) {
+                const T* row = v + (size_t)d * cap;
+                if constexpr (SU == 1) {
+                    x[d][e] = __float_as_uint(row[src[0]]);
+                } else {
+                    x[d][e] = 0;
+#pragma unroll
+                    for (int i = 0; i < SU; ++i) x[d][e] |= (uint32_t)row[src[i]] << (8 * (int)sizeof(T) * i);
+                }
             }
         }
-        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_waitcnt(0);                       // (every source of the chunk is in registers)
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * kMoveThreads + tid;
-            if (j < m) {
+        for (int d = 0; d < ROWS; ++d)
 #pragma unroll
-                for (int d = 0; d < ROWS; ++d) v[(size_t)d * cap + j] = x[u][d];
+            for (int e = 0; e < E; ++e) {
+                const int j = j0 + (e * THREADS + tid) * SU;
+                T* to = v + (size_t)d * cap + j;
+                if (j + SU <= m) {
+                    *reinterpret_cast<typename Word<T>::type*>(to) = x[d][e];
+                } else {
+                    if constexpr (SU > 1) {
+#pragma unroll
+                        for (int i = 0; i < SU; ++i)
+                            if (j + i < m) to[i] = (T)(x[d][e] >> (8 * (int)sizeof(T) * i));
+                    }
+                }
             }
-        }
     }
 }
 
-// Grid: x = parts of a (sequence, KV head): DH bytes-of-K segments, then groups of V rows,
-// then (with sums) one part for them; parts fastest.
-template <typename T, int DH>
-__global__ __launch_bounds__(kMoveThreads) void kv_compact_kernel(KvCompactArgs a) {
-    constexpr int SEG = 64, ROWS = 8, KP = DH * (int)sizeof(T) / SEG, VP = DH / ROWS;
-    const int parts = KP + VP + (a.weights ? 1 : 0), head = blockIdx.x / parts, s = head / a.Hkv;
+// Grid: the parts of every (sequence, KV head), dealt to the XCDs like the key weights'
+// units, so that segments of one line meet in one L2: segments of K's rows, groups of
+// V's rows, then (with sums) one part for them.
+template <typename T, int DH, int THREADS, int SEG, int ROWS, int E>
+__global__ __launch_bounds__(THREADS) void kv_compact_kernel(KvCompactArgs a) {
+    constexpr int KP = DH * (int)sizeof(T) / SEG, VP = DH / ROWS;
+    const int parts = KP + VP + (a.weights ? 1 : 0), heads = a.b * a.Hkv, per = heads >> 3;
+    const int total = gridDim.x, xcd = blockIdx.x & 7, bid = xcd * (total >> 3) + min(xcd, total & 7) + (blockIdx.x >> 3);
+    const int slot = bid / parts, head = heads & 7 ? slot : slot % per * 8 + slot / per, s = head / a.Hkv;
     const int p = prefix_len(a.prefix, s, a.P);
     const int m = min(a.kept ? max(a.kept[s], 0) : a.n, min(a.n, p));
     const int32_t* keep = a.keep + (size_t)head * a.n;
     const size_t base = (size_t)head * a.cap * DH;
-    int part = blockIdx.x % parts;
+    int part = bid % parts;
     if (part < KP) {
-        move_keys<SEG>(reinterpret_cast<char*>(a.k) + base * sizeof(T) + part * SEG, DH * sizeof(T), keep, m, max(p, 1));
+        move_keys<THREADS, SEG>(reinterpret_cast<char*>(a.k) + base * sizeof(T) + part * SEG, DH * sizeof(T), keep, m, p);
         return;
     }
     part -= KP;
     if (part < VP) {
-        move_values<T, ROWS>(reinterpret_cast<T*>(a.v) + base + (size_t)part * ROWS * a.cap, a.cap, keep, m, max(p, 1));
+        move_values<T, THREADS, ROWS, E>(reinterpret_cast<T*>(a.v) + base + (size_t)part * ROWS * a.cap, a.cap, keep, m, p);
         return;
     }
     float* w = a.weights + (size_t)head * a.ldw;
-    move_values<float, 1>(w, 0, keep, m, max(p, 1));
+    move_values<float, THREADS, 1, 4>(w, 0, keep, m, p);
     __syncthreads();
-    for (int j = m + threadIdx.x; j < p; j += kMoveThreads) w[j] = 0.f;   // freed places start from nothing
+    for (int j = m + threadIdx.x; j < p; j += THREADS) w[j] = 0.f;   // freed places start from nothing
 }
 
 }  // namespace
@@ -449,17 +597,25 @@ hipError_t launch_key_weights(int dtype, const KeyWeightArgs& a, hipStream_t s) 
 }
 
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s) {
-    launch(kv_select_kernel, dim3(a.b * a.Hkv), dim3(kSelThreads), 0, s, a);
+    const dim3 grid(a.b * a.Hkv);
+    // (a wave's run is whole 256s: up to kHeld * 64 keys of it are held)
+    if ((a.P + kSelWaves - 1) / kSelWaves <= kHeld * 64) launch(kv_select_kernel<true>, grid, dim3(kSelThreads), 0, s, a);
+    else launch(kv_select_kernel<false>, grid, dim3(kSelThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, int DH, int THREADS, int SEG, int ROWS, int E>
+static hipError_t compact_as(const KvCompactArgs& a, hipStream_t s) {
+    const int parts = DH * (int)sizeof(T) / SEG + DH / ROWS + (a.weights ? 1 : 0);
+    launch(kv_compact_kernel<T, DH, THREADS, SEG, ROWS, E>, dim3((unsigned)((long)parts * a.b * a.Hkv)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t compact(const KvCompactArgs& a, hipStream_t s) {
-    const int parts = a.dh * (int)sizeof(T) / 64 + a.dh / 8 + (a.weights ? 1 : 0);
-    const dim3 grid((unsigned)((long)parts * a.b * a.Hkv));
-    if (a.dh == 128) launch(kv_compact_kernel<T, 128>, grid, dim3(kMoveThreads), 0, s, a);
-    else launch(kv_compact_kernel<T, 64>, grid, dim3(kMoveThreads), 0, s, a);
-    return hipGetLastError();
+    const bool few = (long)a.b * a.Hkv * a.dh < 4096 && a.n > 2048;
+    if (few) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 2, 2>(a, s) : compact_as<T, 64, 1024, 32, 2, 2>(a, s);
+    return a.dh == 128 ? compact_as<T, 128, 256, 64, 8, 1>(a, s) : compact_as<T, 64, 256, 64, 8, 1>(a, s);
 }
 
 hipError_t launch_kv_compact(int dtype, const KvCompactArgs& a, hipStream_t s) {

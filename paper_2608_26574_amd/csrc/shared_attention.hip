@@ -35,18 +35,9 @@ constexpr float kLeast = -3.402823466e38f;
 constexpr float kBig = 256.f;        // a lane's probability sum over a tile that moves the running maximum
 constexpr int kMaxSplit = 32;        // key splits across workgroups
 
-// LDS of one group of TPG threads: three K stages [64 keys][DH] and two V^T
-// stages [DH][64 keys], or, at the end, every lane's o, m and l.
-template <int DH, int TPG>
-struct SLds {
-    static constexpr int TILE = kKeys * DH * 2;
-    static constexpr int MERGE = (DH / 2 + 2) * TPG * 4;
-    static constexpr int GROUP = ((5 * TILE > MERGE ? 5 * TILE : MERGE) + 15) / 16 * 16;
-};
-
 // A tile of the walk: seq < 0 for shared keys, else the sequence (counted from
 // the workgroup's first); keys k0 .. k0 + n - 1 of that cache; p the sequence's
-// prefix length.  Uniform over a workgroup's group.
+// prefix length.  Uniform over the workgroup.
 struct Tile {
     int seq, k0, n, p;
 };
@@ -59,20 +50,19 @@ __device__ __forceinline__ uint64_t own_word(const uint64_t (&x)[kBlockWords], i
     return pre | bits64(x, B, s) | (~bits64(x, B, s - B) & range_mask(s - B, B));
 }
 
-template <int DH, int WAVES, int G, bool KV8>
-__global__ __launch_bounds__(64 * WAVES * G) __attribute__((amdgpu_waves_per_eu(2)))
+// LDS: three K stages [64 keys][DH] and two V^T stages [DH][64 keys].
+template <int DH, int WAVES, bool KV8>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
-    constexpr int TPG = 64 * WAVES, ROWS = 32 * WAVES;
-    constexpr int NCH = kKeys * DH / 8, NI = NCH / TPG;      // 16-byte chunks of a tile, and of a thread
-    static_assert(NCH % TPG == 0 && ROWS <= 128, "whole chunks per thread; at most 64 sequences among the rows");
-    using L = SLds<DH, TPG>;
+    constexpr int ROWS = 32 * WAVES, TILE = kKeys * DH * 2;
+    constexpr int NCH = kKeys * DH / 8, NI = NCH / (64 * WAVES);   // 16-byte chunks of a tile, and of a thread
+    static_assert(NCH % (64 * WAVES) == 0 && ROWS <= 128, "whole chunks per thread; at most 64 sequences among the rows");
     using KVT = typename std::conditional<KV8, uint8_t, bf16_t>::type;
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef __attribute__((address_space(1))) void* glb_ptr;
-    __shared__ __attribute__((aligned(16))) char smem[G * L::GROUP];
+    __shared__ __attribute__((aligned(16))) char smem[5 * TILE];
 
-    const int grp = __builtin_amdgcn_readfirstlane(threadIdx.x / TPG), tid = threadIdx.x % TPG;
-    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 31, eta = lane >> 5;
     // row tile fastest, then key split, then KV head, dealt to the XCDs in
     // contiguous runs: workgroups that read the same keys share an L2
@@ -102,7 +92,6 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     }
     const int ntiles = nsh + __builtin_amdgcn_readlane(upto, 63);
     const int t_begin = (int)((long long)ntiles * split / nsplit), t_end = (int)((long long)ntiles * (split + 1) / nsplit);
-    const int iters = (t_end - t_begin + G - 1) / G;
     auto tile_at = [&](int t) __attribute__((always_inline)) {
         Tile d;
         if (t < nsh) {
@@ -120,82 +109,65 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
         }
         return d;
     };
-    auto mine = [&](int it) __attribute__((always_inline)) { return t_begin + grp + G * it < t_end; };
-    auto at = [&](int it) __attribute__((always_inline)) { return tile_at(t_begin + grp + G * it); };
 
     const KVT* ksh = reinterpret_cast<const KVT*>(a.ksh) + (size_t)kvh * a.cap_sh * DH;
     const KVT* vsh = reinterpret_cast<const KVT*>(a.vsh) + (size_t)kvh * a.cap_sh * DH;
-    char* gbase = smem + grp * L::GROUP;
     auto keys_of = [&](const Tile& d) __attribute__((always_inline)) {
         const KVT* base = d.seq < 0 ? ksh : reinterpret_cast<const KVT*>(a.k) + ((size_t)(s0 + d.seq) * a.Hkv + kvh) * a.cap * DH;
-        return base + (size_t)d.k0 * DH;
+        return reinterpret_cast<const char*>(base + (size_t)d.k0 * DH);
     };
     auto values_of = [&](const Tile& d) __attribute__((always_inline)) {
         const KVT* base = d.seq < 0 ? vsh : reinterpret_cast<const KVT*>(a.v) + ((size_t)(s0 + d.seq) * a.Hkv + kvh) * a.cap * DH;
-        return base + d.k0;
+        return reinterpret_cast<const char*>(base + d.k0);
     };
 
     // ---- copies into LDS.  Chunk q = (wave NI + j) 64 + lane of the swizzled
     // image goes straight there (16 bytes a lane; an FP8 cache goes through
-    // registers and is widened).  Nothing past a tile's n keys is read: K rows past
-    // them are left out (their scores are masked, whatever the stage held), V
-    // chunks past them are zeros, a chunk that straddles n is put together by
-    // elements.
-    auto krc = [&](int j, int& r, int& c) __attribute__((always_inline)) {
-        const int q = (wave * NI + j) * 64 + lane;
-        r = q / (DH / 8);
-        c = (q % (DH / 8)) ^ kswz<DH>(r);
-    };
-    auto vrc = [&](int j, int& d, int& c) __attribute__((always_inline)) {
-        const int q = (wave * NI + j) * 64 + lane;
-        d = q / (kKeys / 8);
-        c = (q % (kKeys / 8)) ^ vswz(d);
+    // registers and is widened).  K rows past a tile's n keys are
+    // left out (their scores are masked, whatever the stage held).  Values past them
+    // come along where the cache holds 64 (their probabilities are 0, and infinities
+    // and NaN are looked for in such tiles); past the cache's end nothing is read.
+    // Addresses are a uniform part and 32 bits of a lane's own.
+    uint32_t koff[NI];                                       // byte of the lane's chunk j in a K tile
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const int q = (wave * NI + j) * 64 + lane, r = q / (DH / 8);
+        koff[j] = (uint32_t)(r * DH + 8 * ((q % (DH / 8)) ^ kswz<DH>(r))) * sizeof(KVT);
+    }
+    auto krow = [&](int j) __attribute__((always_inline)) { return ((wave * NI + j) * 64 + lane) / (DH / 8); };
+    // V chunk j: row d = 8 (wave NI + j) + lane / 8, keys 8 c .. of the tile
+    auto vchunk = [&](int j) __attribute__((always_inline)) { return ((lane & 7) ^ (lane >> 3) ^ (wave * NI + j)) & 7; };
+    auto vrow = [&](const char* vt, int j, int vcap) __attribute__((always_inline)) {
+        return vt + (size_t)(8 * (wave * NI + j)) * vcap * sizeof(KVT);
     };
     uint2 kreg[NI], vreg[NI];
     auto load_k8 = [&](const Tile& t) __attribute__((always_inline)) {
-        const KVT* kt = keys_of(t);
+        const char* kt = keys_of(t);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            int r, c;
-            krc(j, r, c);
-            if (r < t.n) kreg[j] = *reinterpret_cast<const uint2*>(kt + r * DH + 8 * c);
-        }
+        for (int j = 0; j < NI; ++j)
+            if (krow(j) < t.n) kreg[j] = *reinterpret_cast<const uint2*>(kt + koff[j]);
     };
     auto commit_k8 = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            int r, c;
-            krc(j, r, c);
-            if (r < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(kreg[j]);
+            if (krow(j) < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(kreg[j]);
         }
     };
+    // (a V row starts at any byte: cap and the tile's first key may be odd)
+    typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(1)));
+    typedef uint64_t u64x2u __attribute__((ext_vector_type(2), aligned(2)));
     auto load_v8 = [&](const Tile& t) __attribute__((always_inline)) {
-        const KVT* vt = values_of(t);
+        const char* vt = values_of(t);
         const int vcap = t.seq < 0 ? a.cap_sh : a.cap;
-        // (rows of 8-byte chunks that are all aligned: the usual case)
-        if (t.n == kKeys && ((vcap | (int)reinterpret_cast<uintptr_t>(vt)) & 7) == 0) {
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                int d, c;
-                vrc(j, d, c);
-                vreg[j] = *reinterpret_cast<const uint2*>(vt + (size_t)d * vcap + 8 * c);
-            }
-            return;
-        }
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            int d, c;
-            vrc(j, d, c);
-            const KVT* src = vt + (size_t)d * vcap + 8 * c;
-            const int cnt = t.n - 8 * c;                     // keys of the chunk inside the tile
-            uint2 w = make_uint2(0u, 0u);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < cnt) {
-                    const uint32_t bt = (uint32_t)src[e] << (8 * (e & 3));
-                    if (e < 4) w.x |= bt; else w.y |= bt;
-                }
-            vreg[j] = w;
+            const int c = vchunk(j), have = vcap - t.k0 - 8 * c, back = have < 8 ? 8 - have : 0;   // keys of the row from here on
+            uint64_t w = 0;
+            if (back < 8 && vcap >= 8) {
+                const u32x2u x = *reinterpret_cast<const u32x2u*>(vrow(vt, j, vcap) + ((uint32_t)(lane >> 3) * vcap + 8 * c) - back);
+                w = (((uint64_t)x[1] << 32) | x[0]) >> (8 * back);
+            }
+            vreg[j] = make_uint2((uint32_t)w, (uint32_t)(w >> 32));
         }
     };
     auto commit_v8 = [&](char* dst) __attribute__((always_inline)) {
@@ -208,13 +180,11 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
             load_k8(t);
             commit_k8(t, dst);
         } else {
-            const KVT* kt = keys_of(t);
+            const char* kt = keys_of(t);
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                int r, c;
-                krc(j, r, c);
-                if (t.n == kKeys || r < t.n)
-                    __builtin_amdgcn_global_load_lds((glb_ptr)(kt + r * DH + 8 * c), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+                if (t.n == kKeys || krow(j) < t.n)
+                    __builtin_amdgcn_global_load_lds((glb_ptr)(kt + koff[j]), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
             }
         }
     };
@@ -223,31 +193,62 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
             load_v8(t);
             commit_v8(dst);
         } else {
-            const KVT* vt = values_of(t);
+            const char* vt = values_of(t);
             const int vcap = t.seq < 0 ? a.cap_sh : a.cap;
+            const uint32_t row = (uint32_t)(lane >> 3) * vcap * 2;
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                int d, c;
-                vrc(j, d, c);
-                const KVT* src = vt + (size_t)d * vcap + 8 * c;
-                if (t.n == kKeys || 8 * c + 8 <= t.n) {
-                    __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
-                } else {
-                    bf16x8 w = {};
+                const int c = vchunk(j);
+                if (t.k0 + 8 * c + 8 <= vcap)
+                    __builtin_amdgcn_global_load_lds((glb_ptr)(vrow(vt, j, vcap) + (row + 16 * c)), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+            }
+            if (t.k0 + kKeys <= vcap) return;
+            // chunks that pass the cache's end: the last 8 keys of the row, shifted, or zeros
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (8 * c + e < t.n) w[e] = __builtin_bit_cast(__bf16, src[e]);
-                    *reinterpret_cast<bf16x8*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = w;
+            for (int j = 0; j < NI; ++j) {
+                const int c = vchunk(j), back = 8 - (vcap - t.k0 - 8 * c);
+                if (back <= 0) continue;
+                uint64_t lo = 0, hi = 0;
+                if (back < 8 && vcap >= 8) {
+                    const u64x2u x = *reinterpret_cast<const u64x2u*>(vrow(vt, j, vcap) + (row + 16 * c) - 2 * back);
+                    const int sh = 16 * (back & 3);
+                    lo = back >= 4 ? x[1] >> sh : (sh ? (x[0] >> sh) | (x[1] << (64 - sh)) : x[0]);
+                    hi = back >= 4 ? 0 : x[1] >> sh;
                 }
+                *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) =
+                    make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
             }
         }
     };
-    auto kst = [&](int i) __attribute__((always_inline)) { return gbase + (i % 3) * L::TILE; };
-    auto vst = [&](int i) __attribute__((always_inline)) { return gbase + (3 + (i & 1)) * L::TILE; };
-    if (mine(0)) {
-        issue_k(at(0), kst(0));
-        issue_v(at(0), vst(0));
+    // a cache of less than 8 keys has no 8 to read: element by element into the stage (the lane's own
+    // chunks, after what issue_v or commit_v8 wrote there)
+    auto tiny_v = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
+        const int vcap = t.seq < 0 ? a.cap_sh : a.cap;
+        if (vcap >= 8) return;
+        const char* vt = values_of(t);
+#pragma unroll 1
+        for (int j = 0; j < NI; ++j) {
+#pragma unroll 1
+            for (int e = 0; e < t.n && vchunk(j) == 0; ++e) {
+                const KVT x = reinterpret_cast<const KVT*>(vrow(vt, j, vcap))[(lane >> 3) * vcap + e];
+                uint16_t w;
+                if constexpr (KV8) w = (uint16_t)e4m3x2_to_bf16x2<false>(x);
+                else w = x;
+                *reinterpret_cast<uint16_t*>(dst + 16 * ((wave * NI + j) * 64 + lane) + 2 * e) = w;
+            }
+        }
+    };
+    auto kst = [&](int i) __attribute__((always_inline)) { return smem + (i % 3) * TILE; };
+    auto vst = [&](int i) __attribute__((always_inline)) { return smem + (3 + (i & 1)) * TILE; };
+    // tiles of this step, the next and the one after it (none: n = 0)
+    const Tile none = {-1, 0, 0, 0};
+    Tile t0 = t_begin < t_end ? tile_at(t_begin) : none, t1 = t_begin + 1 < t_end ? tile_at(t_begin + 1) : none;
+    if (t0.n) {
+        issue_k(t0, kst(0));
+        issue_v(t0, vst(0));
+        tiny_v(t0, vst(0));
     }
+    if (t1.n) issue_k(t1, kst(1));
 
     // ---- this lane's query row, its Q operand and its take-x words
     const int rho = rt * ROWS + 32 * wave + lr;
@@ -262,9 +263,11 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c)
         qf[c] = ld_bf16x8(reinterpret_cast<const bf16_t*>(a.q) + orow * DH + 16 * c + 8 * eta);
-    // take-x words, read where a tile has block keys (they would hold 8 registers through the loop)
+    // take-x words: the first kept, others read where a tile has block keys (they would
+    // hold 6 registers through the loop)
     const int W = (a.B + 63) / 64;
     const uint64_t* sel = a.sel + ((size_t)seq * R + r) * W;
+    const uint64_t sel0 = sel[0];
     const float sl2 = a.scale * kLog2e;
     // K row pi(lr) of each 32-key block, V^T row lr: operand addresses inside a
     // stage; a chunk or a block of rows further is an XOR or an offset
@@ -312,7 +315,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
             else {
                 uint64_t xw[kBlockWords];
 #pragma unroll
-                for (int q = 0; q < kBlockWords; ++q) xw[q] = q < W ? sel[q] : 0ull;
+                for (int q = 0; q < kBlockWords; ++q) xw[q] = q == 0 ? sel0 : (q < W ? sel[q] : 0ull);
                 vis = seq - s0 == t.seq ? own_word(xw, a.B, t.p, t.k0) : 0ull;
             }
             const uint64_t ww = vis >> (8 * eta);
@@ -359,7 +362,8 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
         if (!whole) {
             // An infinity or NaN among the values of a tile that not every row sees
             // whole must not reach the rows that do not see its key (0 times it is
-            // NaN): such elements leave the product and are added row by row.
+            // NaN), nor may one behind the tile's keys: such elements leave the product
+            // and are added row by row.
             uint32_t top = 0;
 #pragma unroll
             for (int d = 0; d < DH / 32; ++d)
@@ -381,9 +385,12 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
                         for (int e = 0; e < 8; ++e)
                             if ((__builtin_bit_cast(uint16_t, (__bf16)f[e]) & 0x7F80u) == 0x7F80u) f[e] = (__bf16)0.f;
                         o[d] = mfma32x32x16(f, pb[st >> 1][st & 1], o[d]);
+                        __builtin_amdgcn_sched_barrier(0);   // (a rare path: as few registers as it can)
                     }
                 for (int key = 0; key < t.n; ++key) {
                     // the row's probability of this key, from the lane of the row that holds it
+                    const bool sees = (vis >> key) & 1ull;
+                    if (!__ballot(sees)) continue;
                     const int kb = key >> 5, e = (key & 7) + 8 * ((key >> 4) & 1), from = lr + 32 * ((key >> 3) & 1);
                     float pk = 0.f;
 #pragma unroll
@@ -392,14 +399,14 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
                         for (int v = 0; v < 16; ++v)
                             if (b2 == kb && v == e) pk = (float)pb[b2][v >> 3][v & 7];
                     pk = __shfl(pk, from, 64);
-                    const bool sees = (vis >> key) & 1ull;
 #pragma unroll
                     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
                         for (int v = 0; v < 16; ++v) {
                             const int dim = 32 * d + 8 * (v >> 2) + 4 * eta + (v & 3);
                             const bf16_t w = *reinterpret_cast<const bf16_t*>(vs + 16 * vslot(dim, key >> 3) + 2 * (key & 7));
-                            if (sees && (w & 0x7F80u) == 0x7F80u) o[d][v] += pk * bf2f(w);
+                            o[d][v] += sees && (w & 0x7F80u) == 0x7F80u ? pk * bf2f(w) : 0.f;
+                            __builtin_amdgcn_sched_barrier(0);
                         }
                 }
                 return;
@@ -421,94 +428,44 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
         return w_any && (t.seq < 0 || (t.seq >= w_lo && t.seq <= w_hi));
     };
 
-    // ---- main loop: V one step ahead of its use, K two (three for a second group,
-    // which runs half a step out of phase so that on every SIMD one wave's matrix
-    // instructions meet the other's softmax).  A step ends by waiting for every
-    // copy but the newest K tile's and publishing them with the barrier, which also
-    // retires every wave's reads of the stages that the next step overwrites.
-    // Copies complete in order, so V goes first; a ragged K tile issues fewer
-    // copies than the count assumes, so then all are waited for.
-    const bool late = G > 1 && grp == 1;
-    if (mine(1)) issue_k(at(1), kst(1));
-    if (late && mine(2)) issue_k(at(2), kst(2));
+    // ---- main loop: V one step ahead of its use, K two.  A step ends by waiting for
+    // every copy but the newest K tile's and publishing them with the barrier, which
+    // also retires every wave's reads of the stages that the next step overwrites.
+    // Copies complete in order, so V goes first; a ragged K tile issues fewer copies
+    // than the count assumes, so then all are waited for.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    const int lead = late ? 3 : 2;
-    floatx16 sc[2];
-    if constexpr (G > 1) {
-        if (late) {
-            if (mine(0)) {
-                const Tile t = at(0);
-                if (concerns(t)) scores(kst(0), sc);
-            }
-            // (K tile 3 goes over the stage that these scores read)
-            __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));
-        }
-        wg_barrier();
-    }
-    for (int it = 0; it < iters; ++it) {
-        const bool nextv = mine(it + 1), ahead = mine(it + lead);
-        Tile tv = {}, tk = {};
-        if (nextv) {
-            tv = at(it + 1);
-            if constexpr (KV8) load_v8(tv); else issue_v(tv, vst(it + 1));
-        }
-        if (ahead) {
-            tk = at(it + lead);
-            if constexpr (KV8) load_k8(tk); else issue_k(tk, kst(it + lead));
-        }
-        if (!late) {
-            if (mine(it)) {
-                const Tile t = at(it);
-                if (concerns(t)) {
-                    scores(kst(it), sc);
-                    softmax_pv(sc, t, vst(it));
-                }
-            }
+    for (int it = 0; it < t_end - t_begin; ++it) {
+        const Tile t2 = t_begin + it + 2 < t_end ? tile_at(t_begin + it + 2) : none;
+        if constexpr (KV8) {
+            if (t1.n) load_v8(t1);
+            if (t2.n) load_k8(t2);
         } else {
-            if (mine(it)) {
-                const Tile t = at(it);
-                if (concerns(t)) softmax_pv(sc, t, vst(it));
+            if (t1.n) {
+                issue_v(t1, vst(it + 1));
+                tiny_v(t1, vst(it + 1));
             }
-            __builtin_amdgcn_sched_barrier(0);
-            if (nextv && concerns(tv)) scores(kst(it + 1), sc);
+            if (t2.n) issue_k(t2, kst(it + 2));
+        }
+        if (concerns(t0)) {
+            floatx16 sc[2];
+            scores(kst(it), sc);
+            softmax_pv(sc, t0, vst(it));
         }
         if constexpr (KV8) {
-            if (nextv) commit_v8(vst(it + 1));
-            if (ahead) commit_k8(tk, kst(it + lead));
+            if (t1.n) {
+                commit_v8(vst(it + 1));
+                tiny_v(t1, vst(it + 1));
+            }
+            if (t2.n) commit_k8(t2, kst(it + 2));
             __builtin_amdgcn_s_waitcnt(0);
         } else {
-            if (ahead && tk.n == kKeys) __builtin_amdgcn_s_waitcnt(waitcnt_vm(NI));
+            if (t2.n == kKeys) __builtin_amdgcn_s_waitcnt(waitcnt_vm(NI));
             else __builtin_amdgcn_s_waitcnt(0);
         }
         wg_barrier();
-    }
-
-    // ---- merge the groups through LDS (group 0 keeps the result)
-    if constexpr (G > 1) {
-        float* mb = reinterpret_cast<float*>(gbase);
-        if (grp > 0) {
-#pragma unroll
-            for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) mb[(16 * d + v) * TPG + tid] = o[d][v];
-            mb[(DH / 2) * TPG + tid] = m_run;
-            mb[(DH / 2 + 1) * TPG + tid] = l_run;
-        }
-        __syncthreads();
-        if (grp > 0) return;
-#pragma unroll
-        for (int gg = 1; gg < G; ++gg) {
-            const float* ob = reinterpret_cast<const float*>(smem + gg * L::GROUP);
-            const float m2 = ob[(DH / 2) * TPG + tid], M = fmaxf(m_run, m2);
-            const float f0 = __builtin_amdgcn_exp2f(m_run - M), f1 = __builtin_amdgcn_exp2f(m2 - M);
-            l_run = l_run * f0 + ob[(DH / 2 + 1) * TPG + tid] * f1;
-            m_run = M;
-#pragma unroll
-            for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[d][v] = o[d][v] * f0 + ob[(16 * d + v) * TPG + tid] * f1;
-        }
+        t0 = t1;
+        t1 = t2;
     }
 
     // ---- epilogue: the two lanes of a row hold disjoint keys; a lane holds dims
@@ -768,7 +725,7 @@ __global__ __launch_bounds__(64 * kWavesF) void shared_attn_f32_kernel(SharedAtt
 }
 
 struct SharedCfg {
-    int waves, g, rowtiles, ns;
+    int waves, rowtiles, ns;
 };
 
 SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
@@ -776,7 +733,6 @@ SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     const long rows = (long)b * 2 * B * (Hq / Hkv);
     if (dtype == DARD_DTYPE_F32) {
         c.waves = kWavesF;
-        c.g = 1;
         c.rowtiles = (int)((rows + 15) / 16);
         const long wgs = (long)c.rowtiles * Hkv, tiles = ((long)Ps + P + 2 * B) / kKeysF + 1;
         c.ns = (int)std::max<long>(1, std::min<long>(std::min<long>(512 / wgs, tiles / (2 * kWavesF)), kMaxSplit));
@@ -787,7 +743,6 @@ SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     const long wgs = (long)c.rowtiles * Hkv;
     const long RS = 2L * B * (Hq / Hkv), seqs = std::min<long>(b, (32 * c.waves + RS - 1) / RS);
     const long tiles = ((long)Ps + kKeys - 1) / kKeys + seqs * (((long)P + 2 * B + kKeys - 1) / kKeys);
-    c.g = 1;
     c.ns = (int)std::max<long>(1, std::min<long>(std::min<long>(512 / wgs, tiles / 4), kMaxSplit));
     return c;
 }
@@ -808,8 +763,8 @@ static hipError_t launch_shared(int dtype, const SharedAttnArgs& a, hipStream_t 
         launch(shared_attn_f32_kernel<DH>, grid, dim3(64 * kWavesF), 0, s, a, c.rowtiles, c.ns);
     } else {
         const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8;
-        auto k = c.waves == 4 ? (kv8 ? shared_attn_kernel<DH, 4, 1, true> : shared_attn_kernel<DH, 4, 1, false>)
-                              : (kv8 ? shared_attn_kernel<DH, 2, 1, true> : shared_attn_kernel<DH, 2, 1, false>);
+        auto k = c.waves == 4 ? (kv8 ? shared_attn_kernel<DH, 4, true> : shared_attn_kernel<DH, 4, false>)
+                              : (kv8 ? shared_attn_kernel<DH, 2, true> : shared_attn_kernel<DH, 2, false>);
         launch(k, grid, dim3(64 * c.waves), 0, s, a, c.rowtiles, c.ns);
     }
     const hipError_t e = hipGetLastError();
