@@ -34,6 +34,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -3.402823466e38f;
 constexpr float kBig = 256.f;        // a lane's probability sum over a tile that moves the running maximum
 constexpr int kMaxSplit = 32;        // key splits across workgroups
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // A tile of the walk: seq < 0 for shared keys, else the sequence (counted from
 // the workgroup's first); keys k0 .. k0 + n - 1 of that cache; p the sequence's
@@ -140,17 +142,17 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     auto vrow = [&](const char* vt, int j, int vcap) __attribute__((always_inline)) {
         return vt + (size_t)(8 * (wave * NI + j)) * vcap * sizeof(KVT);
     };
-    uint2 kreg[NI], vreg[NI];
+    u32x2 kreg[NI], vreg[NI];
     auto load_k8 = [&](const Tile& t) __attribute__((always_inline)) {
         const char* kt = keys_of(t);
 #pragma unroll
         for (int j = 0; j < NI; ++j)
-            if (krow(j) < t.n) kreg[j] = *reinterpret_cast<const uint2*>(kt + koff[j]);
+            if (krow(j) < t.n) kreg[j] = *reinterpret_cast<const u32x2*>(kt + koff[j]);
     };
     auto commit_k8 = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            if (krow(j) < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(kreg[j]);
+            if (krow(j) < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(make_uint2(kreg[j][0], kreg[j][1]));
         }
     };
     // (a V row starts at any byte: cap and the tile's first key may be odd)
@@ -167,13 +169,13 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
                 const u32x2u x = *reinterpret_cast<const u32x2u*>(vrow(vt, j, vcap) + ((uint32_t)(lane >> 3) * vcap + 8 * c) - back);
                 w = (((uint64_t)x[1] << 32) | x[0]) >> (8 * back);
             }
-            vreg[j] = make_uint2((uint32_t)w, (uint32_t)(w >> 32));
+            vreg[j] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
         }
     };
     auto commit_v8 = [&](char* dst) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
-            *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(vreg[j]);
+            *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(make_uint2(vreg[j][0], vreg[j][1]));
     };
     auto issue_k = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
         if constexpr (KV8) {
@@ -181,11 +183,17 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
             commit_k8(t, dst);
         } else {
             const char* kt = keys_of(t);
+            auto copy = [&](int j) __attribute__((always_inline)) {
+                __builtin_amdgcn_global_load_lds((glb_ptr)(kt + koff[j]), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+            };
+            if (t.n == kKeys) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                if (t.n == kKeys || krow(j) < t.n)
-                    __builtin_amdgcn_global_load_lds((glb_ptr)(kt + koff[j]), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+                for (int j = 0; j < NI; ++j) copy(j);
+                return;
             }
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+                if (krow(j) < t.n) copy(j);
         }
     };
     auto issue_v = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
@@ -196,13 +204,18 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
             const char* vt = values_of(t);
             const int vcap = t.seq < 0 ? a.cap_sh : a.cap;
             const uint32_t row = (uint32_t)(lane >> 3) * vcap * 2;
+            auto copy = [&](int j) __attribute__((always_inline)) {
+                __builtin_amdgcn_global_load_lds((glb_ptr)(vrow(vt, j, vcap) + (row + 16 * vchunk(j))),
+                                                 (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+            };
+            if (t.k0 + kKeys <= vcap) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int c = vchunk(j);
-                if (t.k0 + 8 * c + 8 <= vcap)
-                    __builtin_amdgcn_global_load_lds((glb_ptr)(vrow(vt, j, vcap) + (row + 16 * c)), (lds_ptr)(dst + (wave * NI + j) * 1024), 16, 0, 0);
+                for (int j = 0; j < NI; ++j) copy(j);
+                return;
             }
-            if (t.k0 + kKeys <= vcap) return;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+                if (t.k0 + 8 * vchunk(j) + 8 <= vcap) copy(j);
             // chunks that pass the cache's end: the last 8 keys of the row, shifted, or zeros
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
@@ -359,68 +372,69 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
                 }
         }
         l_run += psum;
+        // An infinity or NaN among the values of a tile that not every row sees whole
+        // must not reach the rows that do not see its key (0 times it is NaN), nor may
+        // one behind the tile's keys: such elements are left out of the product and
+        // added row by row.
+        bool odd = false;
         if (!whole) {
-            // An infinity or NaN among the values of a tile that not every row sees
-            // whole must not reach the rows that do not see its key (0 times it is
-            // NaN), nor may one behind the tile's keys: such elements leave the product
-            // and are added row by row.
             uint32_t top = 0;
 #pragma unroll
             for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
                 for (int st = 0; st < 4; ++st) {
-                    const uint4 w = __builtin_bit_cast(uint4, vfrag(vs, d, st));
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                    const u32x4 w = __builtin_bit_cast(u32x4, vfrag(vs, d, st));
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        top |= ((u[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;   // exponent all ones
+                        top |= ((w[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;   // exponent all ones
                 }
-            if (__ballot(top != 0)) {
-#pragma unroll
-                for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-                    for (int st = 0; st < 4; ++st) {
-                        bf16x8 f = vfrag(vs, d, st);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if ((__builtin_bit_cast(uint16_t, (__bf16)f[e]) & 0x7F80u) == 0x7F80u) f[e] = (__bf16)0.f;
-                        o[d] = mfma32x32x16(f, pb[st >> 1][st & 1], o[d]);
-                        __builtin_amdgcn_sched_barrier(0);   // (a rare path: as few registers as it can)
-                    }
-                for (int key = 0; key < t.n; ++key) {
-                    // the row's probability of this key, from the lane of the row that holds it
-                    const bool sees = (vis >> key) & 1ull;
-                    if (!__ballot(sees)) continue;
-                    const int kb = key >> 5, e = (key & 7) + 8 * ((key >> 4) & 1), from = lr + 32 * ((key >> 3) & 1);
-                    float pk = 0.f;
-#pragma unroll
-                    for (int b2 = 0; b2 < 2; ++b2)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v)
-                            if (b2 == kb && v == e) pk = (float)pb[b2][v >> 3][v & 7];
-                    pk = __shfl(pk, from, 64);
-#pragma unroll
-                    for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const int dim = 32 * d + 8 * (v >> 2) + 4 * eta + (v & 3);
-                            const bf16_t w = *reinterpret_cast<const bf16_t*>(vs + 16 * vslot(dim, key >> 3) + 2 * (key & 7));
-                            o[d][v] += sees && (w & 0x7F80u) == 0x7F80u ? pk * bf2f(w) : 0.f;
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-                }
-                return;
-            }
+            odd = __ballot(top != 0) != 0;
         }
 #pragma unroll
         for (int d = 0; d < DH / 32; ++d) {
             bf16x8 vf[4];
 #pragma unroll
             for (int st = 0; st < 4; ++st) vf[st] = vfrag(vs, d, st);
+            if (odd) {
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    u32x4 w = __builtin_bit_cast(u32x4, vf[st]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t m = ((w[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;   // bit 15 of an odd half
+                        w[e] &= ~(m | (m - (m >> 15)));
+                    }
+                    vf[st] = __builtin_bit_cast(bf16x8, w);
+                }
+            }
 #pragma unroll
             for (int st = 0; st < 4; ++st) o[d] = mfma32x32x16(vf[st], pb[st >> 1][st & 1], o[d]);
             __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        }
+        if (odd) {
+            for (int key = 0; key < t.n; ++key) {
+                const bool sees = (vis >> key) & 1ull;
+                if (!__ballot(sees)) continue;
+                // the row's probability of this key, from the lane of the row that holds it
+                const int kb = key >> 5, e = (key & 7) + 8 * ((key >> 4) & 1), from = lr + 32 * ((key >> 3) & 1);
+                float pk = 0.f;
+#pragma unroll
+                for (int b2 = 0; b2 < 2; ++b2)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (b2 == kb && v == e) pk = (float)pb[b2][v >> 3][v & 7];
+                pk = __shfl(pk, from, 64);
+#pragma unroll
+                for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int dim = 32 * d + 8 * (v >> 2) + 4 * eta + (v & 3);
+                        const bf16_t w = *reinterpret_cast<const bf16_t*>(vs + 16 * vslot(dim, key >> 3) + 2 * (key & 7));
+                        o[d][v] += sees && (w & 0x7F80u) == 0x7F80u ? pk * bf2f(w) : 0.f;
+                        __builtin_amdgcn_sched_barrier(0);   // (a rare path: as few registers as it can)
+                    }
+            }
         }
     };
     // rows of this wave that the tile can concern
