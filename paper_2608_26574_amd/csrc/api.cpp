@@ -647,14 +647,15 @@ int check_shared_attention(int dtype, int b, int B, int Hq, int Hkv, int dh, int
     return DARD_OK;
 }
 
-// Workspace of dard_masked_attention_shared: the state mask (bf16), then the partial results of a key split.
+// Workspace of dard_masked_attention_shared: the state mask (bf16, more than a few positions), then the
+// partial results of a key split.
 struct SharedWs {
     size_t part, total;
 };
 
 SharedWs shared_ws(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P) {
     SharedWs w{};
-    w.part = dtype == DARD_DTYPE_F32 ? 0 : align256((size_t)b * 2 * B * ((B + 63) / 64) * 8);
+    w.part = dtype == DARD_DTYPE_F32 || B <= kSharedFewPositions ? 0 : align256((size_t)b * 2 * B * ((B + 63) / 64) * 8);
     w.total = w.part + shared_attention_partial_floats(dtype, b, B, Hq, Hkv, dh, Ps, P) * 4;
     return w;
 }
@@ -705,7 +706,7 @@ dard_status dard_masked_attention_shared(int dtype, const void* q, const void* k
     a.part = (float*)((char*)ws + w.part);
     hipStream_t s = (hipStream_t)stream;
     TraceScope ts(DARD_K_ATTENTION, s);
-    if (dtype != DARD_DTYPE_F32) {
+    if (w.part) {
         a.sel = (const uint64_t*)ws;
         TraceScope tm(DARD_K_MASK, s);
         HIPOK(launch_build_state_mask(state, conf, b, B, flags, (uint64_t*)ws, s));

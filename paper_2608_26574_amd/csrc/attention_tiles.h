@@ -8,6 +8,15 @@ namespace dard {
 
 constexpr int kKeys = 64;      // keys per tile
 
+// Eight E4M3 codes (two dwords) -> eight bf16 values, two an instruction (exact:
+// at most 4 significant bits, scale 1; a NaN code gives NaN).
+__device__ __forceinline__ uint4 e4m3x8_to_bf16x8_scaled(uint32_t lo, uint32_t hi) {
+    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true)));
+}
+
 // 16-byte chunk slots.  The LDS serves a 16-byte read 16 consecutive lanes
 // per cycle over 64 banks (256 bytes; measured: an image that separates only
 // groups of 8 lanes within 128 bytes kept its conflicts), and each group must

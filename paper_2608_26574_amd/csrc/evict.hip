@@ -104,8 +104,8 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
 #pragma unroll
             for (int c = 0; c < NC; c += 2) {
                 const uint4 w = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(a.k) + row + 8 * ch(c));
-                kf[kb][c] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8(make_uint2(w.x, w.y)));
-                kf[kb][c + 1] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8(make_uint2(w.z, w.w)));
+                kf[kb][c] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8_scaled(w.x, w.y));
+                kf[kb][c + 1] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8_scaled(w.z, w.w));
             }
         } else {
 #pragma unroll

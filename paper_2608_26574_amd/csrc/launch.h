@@ -66,14 +66,16 @@ struct SharedAttnArgs {
     float* lse;                           // [b][2B][Hq], or NULL
     const void* ksh; const void* vsh;     // [Hkv][cap_sh][dh], [Hkv][dh][cap_sh]: keys 0 .. Ps - 1 of every sequence
     const void* k; const void* v;         // [b][Hkv][cap][dh], [b][Hkv][dh][cap]: own prefix, then the block
-    const uint8_t* state; const float* conf;   // [b][B] (fp32)
-    const uint64_t* sel;                  // [b][2B][ceil(B / 64)] take-x words (bf16)
+    const uint8_t* state; const float* conf;   // [b][B]
+    const uint64_t* sel;                  // [b][2B][ceil(B / 64)] take-x words (bf16, more than
+                                          // kSharedFewPositions positions; else not read)
     const int32_t* prefix;                // [b] own prefix lengths (clamped to [0, P]), or NULL: P
     int Ps, cap_sh, P, cap, b, B, Hq, Hkv, dh;
     float scale;
     uint32_t flags;
     float* part;                          // key-split partials (shared_attention_partial_floats)
 };
+constexpr int kSharedFewPositions = 16;   // blocks whose state mask the bf16 kernel works out itself
 size_t shared_attention_partial_floats(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P);
 hipError_t launch_shared_attention(int dtype, const SharedAttnArgs& a, hipStream_t s);
 

@@ -11,7 +11,7 @@
 // in LDS serves rows of as many sequences as fit: one position a sequence (two
 // rows) fills matrix tiles that a launch per sequence would leave empty, and the
 // shared keys are read once for 128 rows instead of once for two.  A workgroup
-// takes 32 WAVES consecutive rows and walks the shared tiles, then the own tiles
+// takes 128 consecutive rows and walks the shared tiles, then the own tiles
 // of each sequence among its rows; waves without rows of that sequence leave the
 // tile out.  An own tile is 64 consecutive keys of a sequence's prefix and
 // block, and one 64-bit word per row says which of them the row sees.
@@ -34,6 +34,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -3.402823466e38f;
 constexpr float kBig = 256.f;        // a lane's probability sum over a tile that moves the running maximum
 constexpr int kMaxSplit = 32;        // key splits across workgroups
+constexpr int kFewPositions = kSharedFewPositions;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -53,16 +54,18 @@ __device__ __forceinline__ uint64_t own_word(const uint64_t (&x)[kBlockWords], i
 }
 
 // LDS: three K stages [64 keys][DH] and two V^T stages [DH][64 keys].
-template <int DH, int WAVES, bool KV8>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
+constexpr int kWaves = 4, kRows = 32 * kWaves;   // of a workgroup
+
+template <int DH, bool KV8>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
-    constexpr int ROWS = 32 * WAVES, TILE = kKeys * DH * 2;
-    constexpr int NCH = kKeys * DH / 8, NI = NCH / (64 * WAVES);   // 16-byte chunks of a tile, and of a thread
-    static_assert(NCH % (64 * WAVES) == 0 && ROWS <= 128, "whole chunks per thread; at most 64 sequences among the rows");
+    constexpr int ROWS = kRows, TILE = kKeys * DH * 2;
+    constexpr int NI = kKeys * DH / 8 / (64 * kWaves);       // 16-byte chunks of a tile that a thread copies
+    static_assert(ROWS <= 128, "at most 64 sequences among the rows");
     using KVT = typename std::conditional<KV8, uint8_t, bf16_t>::type;
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef __attribute__((address_space(1))) void* glb_ptr;
-    __shared__ __attribute__((aligned(16))) char smem[5 * TILE];
+    __shared__ __attribute__((aligned(16))) char smem[5 * TILE];   // (and the rows' results on their way out)
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lr = lane & 31, eta = lane >> 5;
@@ -80,7 +83,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     // ---- the walk: shared tiles, then the own tiles of sequences s0 ..; lane i
     // holds the prefix length of sequence s0 + i and the own tiles up to it
     const int s0 = rt * ROWS / RS;
-    const int nseq = (min(rt * ROWS + ROWS, total_rows) - 1) / RS - s0 + 1;   // at most 64: RS >= 2 and ROWS <= 128
+    const int nseq = (min(rt * ROWS + ROWS, total_rows) - 1) / RS - s0 + 1;   // at most 64: RS >= 2
     const int nsh = (a.Ps + kKeys - 1) / kKeys;
     int plen = 0, upto = 0;
     if (lane < nseq) {
@@ -152,7 +155,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     auto commit_k8 = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            if (krow(j) < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(make_uint2(kreg[j][0], kreg[j][1]));
+            if (krow(j) < t.n) *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8_scaled(kreg[j][0], kreg[j][1]);
         }
     };
     // (a V row starts at any byte: cap and the tile's first key may be odd)
@@ -175,7 +178,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     auto commit_v8 = [&](char* dst) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NI; ++j)
-            *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8(make_uint2(vreg[j][0], vreg[j][1]));
+            *reinterpret_cast<uint4*>(dst + 16 * ((wave * NI + j) * 64 + lane)) = e4m3x8_to_bf16x8_scaled(vreg[j][0], vreg[j][1]);
     };
     auto issue_k = [&](const Tile& t, char* dst) __attribute__((always_inline)) {
         if constexpr (KV8) {
@@ -277,10 +280,23 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     for (int c = 0; c < DH / 16; ++c)
         qf[c] = ld_bf16x8(reinterpret_cast<const bf16_t*>(a.q) + orow * DH + 16 * c + 8 * eta);
     // take-x words: the first kept, others read where a tile has block keys (they would
-    // hold 6 registers through the loop)
+    // hold 6 registers through the loop).  Few positions: worked out here, behind the
+    // first copies (a kernel of their own takes 3 to 4 us); the wave's sequences have at
+    // most 16 / GQ + 2 B <= 48 of them, one a lane
     const int W = (a.B + 63) / 64;
     const uint64_t* sel = a.sel + ((size_t)seq * R + r) * W;
-    const uint64_t sel0 = sel[0];
+    uint64_t sel0 = 0;
+    if (a.B > kFewPositions) {
+        sel0 = sel[0];
+    } else if (t_end > nsh) {
+        const int at = min((s0 + w_lo) * a.B + lane, a.b * a.B - 1);
+        const int st = a.state[at];
+        const float cf = a.conf[at];
+        const int base = (seq - s0 - w_lo) * a.B, i = r % a.B, si = __shfl(st, base + i, 64);
+        const float ci = __shfl(cf, base + i, 64);
+        for (int j = 0; j < a.B; ++j)
+            if (take_x(si, __shfl(st, base + j, 64), ci, __shfl(cf, base + j, 64), i, j, r >= a.B, a.flags)) sel0 |= 1ull << j;
+    }
     const float sl2 = a.scale * kLog2e;
     // K row pi(lr) of each 32-key block, V^T row lr: operand addresses inside a
     // stage; a chunk or a block of rows further is an XOR or an offset
@@ -295,21 +311,26 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
 
     // S^T = K Q^T: value v of block kb is key 32 kb + 16 (v / 8) + 8 eta + v % 8
     auto scores = [&](const char* ks, floatx16 (&sc)[2]) __attribute__((always_inline)) {
-        constexpr int NC = DH / 16;
+        // (two chains of products in turn; operand reads run eight ahead)
+        constexpr int NF = DH / 8;
         const uint32_t kb0 = (uint32_t)(ks - smem) + kaddr0;
+        bf16x8 kf[NF];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            bf16x8 kf[NC];
+        for (int i = 0; i < NF; ++i)
+            kf[i] = *reinterpret_cast<const bf16x8*>(smem + ((kb0 ^ (32u * (i >> 1))) + (i & 1) * 32 * DH * 2));
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                kf[c] = *reinterpret_cast<const bf16x8*>(smem + ((kb0 ^ (32u * c)) + kb * 32 * DH * 2));
+        for (int v = 0; v < 16; ++v) sc[0][v] = sc[1][v] = 0.f;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sc[kb][v] = 0.f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) sc[kb] = mfma32x32x16(kf[c], qf[c], sc[kb]);
-            __builtin_amdgcn_sched_group_barrier(0x100, NC, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, NC, 0);
+        for (int i = 0; i < NF; ++i) sc[i & 1] = mfma32x32x16(kf[i], qf[i >> 1], sc[i & 1]);
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        if constexpr (NF == 16) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     };
     auto vfrag = [&](const char* vs, int d, int st) __attribute__((always_inline)) {
         const uint32_t vb0 = (uint32_t)(vs - smem) + vaddr0;
@@ -483,39 +504,55 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     }
 
     // ---- epilogue: the two lanes of a row hold disjoint keys; a lane holds dims
-    // 32 d + 8 j + 4 eta + {0..3}
+    // 32 d + 8 j + 4 eta + {0..3}.  Rows go out through the wave's part of the LDS, so
+    // that a store covers whole rows (16-byte pieces of 32 rows at a time took 7 us
+    // of a call with 512 workgroups); chunk c of row r sits in slot c ^ r.
     const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    if (!row_ok) return;
-    if (nsplit == 1) {
-        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;  // (every score minus infinity: zeros)
-        bf16_t* out = reinterpret_cast<bf16_t*>(a.out) + orow * DH;
-#pragma unroll
-        for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                bf16x4 w;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = (__bf16)(o[d][4 * j + e] * inv);
-                *reinterpret_cast<bf16x4*>(out + 32 * d + 8 * j + 4 * eta) = w;
-            }
-        if (a.lse && eta == 0) a.lse[orow] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
-        return;
-    }
-    const size_t nrow = (size_t)total_rows * a.Hkv;          // (b R Hq)
-    float* po = a.part + ((size_t)split * nrow + orow) * DH;
+    const bool whole = nsplit == 1;
+    const float inv = !whole ? 1.f : (l_tot == 0.f ? 0.f : 1.f / l_tot);   // (every score minus infinity: zeros)
+    constexpr int FCH = DH / 4;                              // 16-byte chunks of a row in fp32
+    char* own = smem + wave * 32 * DH * 4;
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<float4*>(po + 32 * d + 8 * j + 4 * eta) =
-                make_float4(o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]);
-    if (eta == 0)
-        *reinterpret_cast<float2*>(a.part + (size_t)nsplit * nrow * DH + ((size_t)split * nrow + orow) * 2) = make_float2(m_run, l_tot);
+        for (int j = 0; j < 4; ++j) {
+            const int c = 8 * d + 2 * j + eta;
+            *reinterpret_cast<floatx4*>(own + 16 * (lr * FCH + (c ^ (lr & (FCH - 1))))) =
+                floatx4{o[d][4 * j] * inv, o[d][4 * j + 1] * inv, o[d][4 * j + 2] * inv, o[d][4 * j + 3] * inv};
+        }
+    const size_t nrow = (size_t)total_rows * a.Hkv;          // (b R Hq)
+    if (eta == 0 && row_ok) {
+        if (!whole)
+            *reinterpret_cast<float2*>(a.part + (size_t)nsplit * nrow * DH + ((size_t)split * nrow + orow) * 2) = make_float2(m_run, l_tot);
+        else if (a.lse)
+            a.lse[orow] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
+    }
+    // a lane takes 8 values of a row, the row's place from the row's own lane
+    constexpr int EPL = DH / 8, RPP = 64 / EPL;              // lanes a row (8 values each), rows a pass
+    const int c8 = lane % EPL;
+#pragma unroll
+    for (int i = 0; i < 32 / RPP; ++i) {
+        const int row = i * RPP + lane / EPL;
+        const floatx4 x = *reinterpret_cast<const floatx4*>(own + 16 * (row * FCH + ((2 * c8) ^ (row & (FCH - 1)))));
+        const floatx4 y = *reinterpret_cast<const floatx4*>(own + 16 * (row * FCH + ((2 * c8 + 1) ^ (row & (FCH - 1)))));
+        const uint32_t to = __shfl((uint32_t)orow, row, 64);  // (rows times heads are under 2^31)
+        if (rt * ROWS + 32 * wave + row >= total_rows) continue;
+        if (whole) {
+            bf16x8 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { w[e] = (__bf16)x[e]; w[4 + e] = (__bf16)y[e]; }
+            *reinterpret_cast<bf16x8*>(reinterpret_cast<bf16_t*>(a.out) + (size_t)to * DH + 8 * c8) = w;
+        } else {
+            float* po = a.part + ((size_t)split * nrow + to) * DH + 8 * c8;
+            *reinterpret_cast<floatx4*>(po) = x;
+            *reinterpret_cast<floatx4*>(po + 4) = y;
+        }
+    }
 }
 
 // Merge of key splits: out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M) in
-// split order.  A thread per (row, head, 4 dims).
+// split order, eight at a time (their loads go out together).  A thread per (row,
+// head, 4 dims).
 template <int DH, typename T>
 __global__ __launch_bounds__(256) void shared_attn_combine_kernel(const float* __restrict__ part, int ns, size_t nrow,
                                                                   T* __restrict__ out, float* __restrict__ lse) {
@@ -523,16 +560,31 @@ __global__ __launch_bounds__(256) void shared_attn_combine_kernel(const float* _
     const int q4 = t % (DH / 4);
     if (row >= nrow) return;
     const float2* ml = reinterpret_cast<const float2*>(part + (size_t)ns * nrow * DH);
-    float M = kLeast;
-    for (int s = 0; s < ns; ++s) M = fmaxf(M, ml[s * nrow + row].x);
-    float l = 0.f;
+    float M = kLeast, l = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < ns; ++s) {
-        const float2 v = ml[s * nrow + row];
-        const float f = __builtin_amdgcn_exp2f(v.x - M);
-        l += v.y * f;
-        acc += reinterpret_cast<const floatx4*>(part + (s * nrow + row) * DH)[q4] * f;
+    for (int s = 0; s < ns; s += 8) {
+        float2 v[8];
+        floatx4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int at = min(s + i, ns - 1);
+            v[i] = ml[at * nrow + row];
+            x[i] = reinterpret_cast<const floatx4*>(part + (at * nrow + row) * DH)[q4];
+        }
+        float top = M;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].x);
+        const float f0 = __builtin_amdgcn_exp2f(M - top);
+        l *= f0;
+        acc *= f0;
+        M = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (s + i < ns) {
+                const float f = __builtin_amdgcn_exp2f(v[i].x - M);
+                l += v[i].y * f;
+                acc += x[i] * f;
+            }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if constexpr (sizeof(T) == 2) {
@@ -739,25 +791,32 @@ __global__ __launch_bounds__(64 * kWavesF) void shared_attn_f32_kernel(SharedAtt
 }
 
 struct SharedCfg {
-    int waves, rowtiles, ns;
+    int rowtiles, ns;
 };
 
+// Key splits: the count of least estimated time.  A workgroup takes 5 us to start and
+// end and t us a tile (bf16: 1.6 alone on its CU, 2.4 for each of two; fp32: its four
+// waves a tile each in 2.5), a split 4 us for the merge and 1040 bytes a row written
+// and read at 5 TB/s.  Measured: 1024 rows x 32 heads, 36 tiles: 67 us whole, 66 in
+// two; 128 x 32, 28 tiles: 28 us in 7, 29 in 14; 16 x 32, 13 tiles: 14 us in 13, 17 in 6.
 SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     SharedCfg c{};
-    const long rows = (long)b * 2 * B * (Hq / Hkv);
-    if (dtype == DARD_DTYPE_F32) {
-        c.waves = kWavesF;
-        c.rowtiles = (int)((rows + 15) / 16);
-        const long wgs = (long)c.rowtiles * Hkv, tiles = ((long)Ps + P + 2 * B) / kKeysF + 1;
-        c.ns = (int)std::max<long>(1, std::min<long>(std::min<long>(512 / wgs, tiles / (2 * kWavesF)), kMaxSplit));
-        return c;
+    const long rows = (long)b * 2 * B * (Hq / Hkv), RS = 2L * B * (Hq / Hkv);
+    const bool f32 = dtype == DARD_DTYPE_F32;
+    const long per = f32 ? 16 : kRows, keys = f32 ? kKeysF : kKeys, step = f32 ? kWavesF : 1;
+    c.rowtiles = (int)((rows + per - 1) / per);
+    const long wgs = (long)c.rowtiles * Hkv, fit = f32 ? 256 : 512;
+    const long seqs = std::min<long>(b, (per + RS - 1) / RS);
+    const long tiles = ((long)Ps + keys - 1) / keys + seqs * (((long)P + 2 * B + keys - 1) / keys);
+    double best = 0;
+    for (long ns = 1; ns <= kMaxSplit && (ns == 1 || (ns * wgs <= fit && ns * step <= tiles)); ++ns) {
+        const double t = f32 ? 2.5 : ns * wgs <= 256 ? 1.6 : 2.4;
+        const double us = (double)((tiles + ns * step - 1) / (ns * step)) * t + (ns > 1 ? 4 + (double)ns * rows * Hkv * 0.00021 : 0);
+        if (ns == 1 || us < best) {
+            best = us;
+            c.ns = (int)ns;
+        }
     }
-    c.waves = rows > 64 ? 4 : 2;
-    c.rowtiles = (int)((rows + 32 * c.waves - 1) / (32 * c.waves));
-    const long wgs = (long)c.rowtiles * Hkv;
-    const long RS = 2L * B * (Hq / Hkv), seqs = std::min<long>(b, (32 * c.waves + RS - 1) / RS);
-    const long tiles = ((long)Ps + kKeys - 1) / kKeys + seqs * (((long)P + 2 * B + kKeys - 1) / kKeys);
-    c.ns = (int)std::max<long>(1, std::min<long>(std::min<long>(512 / wgs, tiles / 4), kMaxSplit));
     return c;
 }
 
@@ -777,9 +836,7 @@ static hipError_t launch_shared(int dtype, const SharedAttnArgs& a, hipStream_t 
         launch(shared_attn_f32_kernel<DH>, grid, dim3(64 * kWavesF), 0, s, a, c.rowtiles, c.ns);
     } else {
         const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8;
-        auto k = c.waves == 4 ? (kv8 ? shared_attn_kernel<DH, 4, true> : shared_attn_kernel<DH, 4, false>)
-                              : (kv8 ? shared_attn_kernel<DH, 2, true> : shared_attn_kernel<DH, 2, false>);
-        launch(k, grid, dim3(64 * c.waves), 0, s, a, c.rowtiles, c.ns);
+        launch(kv8 ? shared_attn_kernel<DH, true> : shared_attn_kernel<DH, false>, grid, dim3(64 * kWaves), 0, s, a, c.rowtiles, c.ns);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.ns == 1) return e;

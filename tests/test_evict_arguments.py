@@ -30,12 +30,12 @@ def attention(**kw):
     (-1, dict(out=None)), (-1, dict(ks=None)), (-1, dict(vs=None)), (-1, dict(dtype=7)), (-1, dict(dtype=-1)),
     (-1, dict(scale=0.0)), (-1, dict(scale=-1.0)), (-1, dict(scale=NAN)), (-1, dict(scale=INF)), (-1, dict(scale=2.0 ** 127)),
     (-1, dict(flags=1 << 20)), (-1, dict(flags=16 | 32)), (-1, dict(q=ODD)), (-1, dict(out=ODD)), (-1, dict(k=ODD)),
-    (-1, dict(v=ODD)), (-1, dict(ks=ODD)), (-1, dict(vs=ODD)), (-1, dict(lse=ODD)), (-1, dict(prefix=ODD)), (-1, dict(ws=ODD)),
+    (-1, dict(v=ODD)), (-1, dict(ks=ODD)), (-1, dict(vs=ODD)), (-1, dict(lse=ODD)), (-1, dict(prefix=ODD)), (-1, dict(ws=ODD, B=20, cap=64)),
     (-1, dict(dtype=0, q=ODD)),
     (-2, dict(b=0)), (-2, dict(B=0)), (-2, dict(B=257, cap=4096)), (-2, dict(Hq=0)), (-2, dict(Hkv=0)), (-2, dict(Hq=3)),
     (-2, dict(dh=96)), (-2, dict(Ps=-1)), (-2, dict(P=-1)), (-2, dict(Ps=11)), (-2, dict(cap=11)), (-2, dict(P=5)),
     (-2, dict(P=2 ** 30 + 1, cap=2 ** 31 - 1)), (-2, dict(Ps=2 ** 30 + 1, cap_sh=2 ** 31 - 1)), (-2, dict(b=2 ** 27)),
-    (-2, dict(P=2 ** 31 - 1, cap=2 ** 31 - 1)), (-5, dict(ws=None)), (-5, dict(n=8))])
+    (-2, dict(P=2 ** 31 - 1, cap=2 ** 31 - 1)), (-5, dict(ws=None, B=20, cap=64)), (-5, dict(n=8, B=20, cap=64))])
 def test_attention_refusals(status, kw):
     assert attention(**kw) == status and dard.lib().dard_last_error()
 
@@ -43,7 +43,7 @@ def test_attention_refusals(status, kw):
 def test_attention_workspace():
     f = dard.lib().dard_attention_shared_workspace_bytes
     assert f(1, 0, 4, 4, 4, 64, 0, 0) == 0 and f(9, 1, 4, 4, 4, 64, 0, 0) == 0 and f(1, 1, 4, 4, 3, 64, 0, 0) == 0
-    assert f(1, 1, 1, 1, 1, 64, 0, 0) >= 2 * 8                       # the state mask
+    assert f(1, 1, 17, 1, 1, 64, 0, 0) >= 34 * 8                     # the state mask
     assert f(0, 1, 1, 1, 1, 64, 0, 0) == 0
     long = f(1, 1, 1, 1, 1, 64, 1 << 20, 0)                          # one row, many keys: split
     assert long > 2 * 2 * 66 * 4
