@@ -743,24 +743,35 @@ dard_status dard_key_weights(int dtype, const void* q, const float* lse, const v
     return DARD_OK;
 }
 
+namespace {
+
+int check_select(int b, int Hkv, int P, int n) {
+    if (b < 1 || Hkv < 1 || P < 0 || n < 1) return fail(DARD_ERR_SHAPE, "need b, Hkv, n >= 1 and P >= 0");
+    if ((double)b * Hkv >= 4194304.0) return fail(DARD_ERR_SHAPE, "too many heads in one call");
+    return DARD_OK;
+}
+
+}  // namespace
+
 size_t dard_kv_select_workspace_bytes(int b, int Hkv, int P, int n) {
-    (void)b; (void)Hkv; (void)P; (void)n;
-    return 0;
+    return check_select(b, Hkv, P, n) ? 0 : kv_select_workspace(b, Hkv, P);
 }
 
 dard_status dard_kv_select(const float* weights, int64_t ldw, int P, const int32_t* prefix, int b, int Hkv, int n, int first,
                            int last, int32_t* keep, int32_t* kept, void* ws, size_t ws_bytes, void* stream) {
     if (!weights || !keep) return fail(DARD_ERR_ARG, "NULL pointer");
-    if (b < 1 || Hkv < 1 || P < 0 || n < 1 || ldw < P) return fail(DARD_ERR_SHAPE, "need b, Hkv, n >= 1 and 0 <= P <= ldw");
+    if (int rc = check_select(b, Hkv, P, n)) return rc;
+    if (ldw < P) return fail(DARD_ERR_SHAPE, "P must be <= ldw");
     if (first < 0 || last < 0 || first > n || last > n - first)
         return fail(DARD_ERR_SHAPE, "need first, last >= 0 and first + last <= n");
-    if ((double)b * Hkv >= 4194304.0 || (double)b * Hkv * n > 1099511627776.0) return fail(DARD_ERR_SHAPE, "too many heads in one call");
     if (!aligned(weights, 4) || !aligned(prefix, 4) || !aligned(keep, 4) || !aligned(kept, 4))
         return fail(DARD_ERR_ARG, "tensors must be 4-byte aligned");
-    (void)ws; (void)ws_bytes;
+    const size_t need = kv_select_workspace(b, Hkv, P);
+    if (need && (!ws || ws_bytes < need)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", need);
+    if (need && !aligned(ws, 16)) return fail(DARD_ERR_ARG, "the workspace must be 16-byte aligned");
     KvSelectArgs a{};
     a.weights = weights; a.ldw = ldw; a.prefix = prefix; a.keep = keep; a.kept = kept;
-    a.b = b; a.Hkv = Hkv; a.P = P; a.n = n; a.first = first; a.last = last;
+    a.b = b; a.Hkv = Hkv; a.P = P; a.n = n; a.first = first; a.last = last; a.ws = (uint32_t*)ws;
     HIPOK(launch_kv_select(a, (hipStream_t)stream));
     return DARD_OK;
 }

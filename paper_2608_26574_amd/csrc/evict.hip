@@ -300,11 +300,9 @@ __device__ __forceinline__ uint32_t sum_rank(float w) {
     return (u >> 31) ? ~u : u | 0x80000000u;                 // -inf: 0x007FFFFF; +inf: 0xFF800000
 }
 
-// HELD: the row's sums fit the registers (kHeld keys a thread) and are read once;
-// else every pass reads them again, 16 keys a thread in flight.
-constexpr int kHeld = 8;
-
-template <bool HELD>
+// HELD: the row's sums fit the registers (HELD keys a thread) and are read once; 0:
+// every pass reads them again, 16 keys a thread in flight.
+template <int HELD>
 __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) {
     // histogram copies by lane: equal sums in neighbouring lanes would queue at one counter
     constexpr int COPIES = 4;
@@ -335,10 +333,10 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
     auto rank = [&](float x, int j) __attribute__((always_inline)) {
         return j < a.first || j >= p - a.last ? 0xFFFFFFFFu : sum_rank(x);
     };
-    floatx4 held[kHeld / 4];
-    if constexpr (HELD) {
+    floatx4 held[HELD ? HELD / 4 : 1];
+    if constexpr (HELD > 0) {
 #pragma unroll
-        for (int i = 0; i < kHeld / 4; ++i) held[i] = fetch(j0 + 256 * i + 4 * lane);
+        for (int i = 0; i < HELD / 4; ++i) held[i] = fetch(j0 + 256 * i + 4 * lane);
     }
     // f(ranks of four keys, index of the first) over the wave's run, in order
     auto run = [&](auto f) __attribute__((always_inline)) {
@@ -348,9 +346,9 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
             for (int e = 0; e < 4; ++e) u[e] = rank(x[e], j + e);
             f(u, j);
         };
-        if constexpr (HELD) {
+        if constexpr (HELD > 0) {
 #pragma unroll
-            for (int i = 0; i < kHeld / 4; ++i)
+            for (int i = 0; i < HELD / 4; ++i)
                 if (j0 + 256 * i < j1) four(held[i], j0 + 256 * i + 4 * lane);
         } else {
             for (int j = j0; j < j1; j += 1024) {
@@ -443,6 +441,178 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
     });
 }
 
+// Long rows of few heads: every digit's histogram, and the indices, in a launch of
+// their own with a workgroup per chunk of kChunk keys.  A workgroup adds the chunks'
+// histograms of the digit before to find the threshold's bin, as each of the others
+// does (nothing has to be initialised, or to meet), and the first one leaves it for
+// the launches to come; so does each its own chunk's count above the threshold so far.
+// From those counts follows where its indices go.
+constexpr int kChunkKeys = 16;                               // keys a thread
+constexpr int kChunk = kSelThreads * kChunkKeys, kBins = 2048;
+
+__global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArgs a, int chunks, int digit) {
+    constexpr int COPIES = 4;                                // (by lane, as in kv_select_kernel)
+    __shared__ uint32_t hist[COPIES][kBins];
+    __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
+    __shared__ uint32_t found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks, s = row / a.Hkv;
+    const int p = prefix_len(a.prefix, s, a.P), m = min(a.n, p), last = digit == 3;
+    int32_t* keep = a.keep + (size_t)row * a.n;
+    const int c0 = chunk * kChunk;
+    if (last) {
+        if (a.kept && row % a.Hkv == 0 && chunk == 0 && tid == 0) a.kept[s] = m;
+        for (int i = max(m, c0) + tid; i < min(a.n, chunk + 1 == chunks ? a.n : c0 + kChunk); i += kSelThreads) keep[i] = -1;
+        if (m == p)
+            for (int i = c0 + tid; i < min(m, c0 + kChunk); i += kSelThreads) keep[i] = i;
+    }
+    if (m == p || c0 >= p) return;
+    // this wave's keys: whole 256s in a row, four neighbours a lane
+    const int j0 = c0 + wave * 64 * kChunkKeys;
+    uint32_t u[kChunkKeys];
+    bool in[kChunkKeys];
+    {
+        const float* w = a.weights + (size_t)row * a.ldw;
+        floatx4 x[kChunkKeys / 4];
+#pragma unroll
+        for (int i = 0; i < kChunkKeys / 4; ++i) {
+            const int j = j0 + 256 * i + 4 * lane;
+            x[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            if (j + 4 <= p) x[i] = ld_f4(w + j);
+            else if (j < p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[i][e] = w[min(j + e, p - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < kChunkKeys; ++i) {
+            const int j = j0 + 256 * (i >> 2) + 4 * lane + (i & 3);
+            in[i] = j < p;
+            u[i] = j < a.first || j >= p - a.last ? 0xFFFFFFFFu : sum_rank(x[i >> 2][i & 3]);
+        }
+    }
+    const int rows = gridDim.x / chunks;
+    uint32_t* state = a.ws + (size_t)3 * gridDim.x * kBins;  // [digit][row]: bin, keys above it; then [digit][row][chunk] counts
+    uint32_t* counts = state + (size_t)6 * rows;
+    uint32_t T = 0, mask = 0, pos = 0, tie = 0;              // pos, tie: keys above T, and ties, of the chunks before this one
+    int need = m;
+    for (int d = 0; d < digit; ++d) {
+        const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bits = d == 2 ? 10 : 11;
+        uint32_t bin, over;
+        if (d + 1 < digit) {
+            const uint2 v = reinterpret_cast<const uint2*>(state)[(size_t)d * rows + row];
+            bin = v.x;
+            over = v.y;
+            if (last)
+                for (int c = 0; c < chunk; ++c) pos += counts[((size_t)d * rows + row) * chunks + c];
+        } else {
+            // this thread's two bins, from the top; their counts in this chunk and in those before it
+            const uint32_t* h = a.ws + ((size_t)d * gridDim.x + (size_t)row * chunks) * kBins + 2046 - 2 * tid;
+            uint32_t n0 = 0, n1 = 0, b0 = 0, b1 = 0, o0 = 0, o1 = 0;
+#pragma unroll 4
+            for (int c = 0; c * kChunk < p; ++c) {
+                const uint2 v = *reinterpret_cast<const uint2*>(h + (size_t)c * kBins);
+                n0 += v.y;
+                n1 += v.x;
+                b0 += c < chunk ? v.y : 0u;
+                b1 += c < chunk ? v.x : 0u;
+                o0 += c == chunk ? v.y : 0u;
+                o1 += c == chunk ? v.x : 0u;
+            }
+            uint32_t sum = n0 + n1;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t below = __shfl_up(sum, o, 64);
+                if (lane >= o) sum += below;
+            }
+            if (lane == 63) wsum[wave] = sum;
+            __syncthreads();
+            uint32_t before = sum - n0 - n1;
+#pragma unroll
+            for (int i = 0; i < kSelWaves; ++i) before += i < wave ? wsum[i] : 0u;
+            const uint32_t want = (uint32_t)need;
+            if (before < want && before + n0 >= want) { found[0] = 2047 - 2 * tid; found[1] = before; }
+            if (before + n0 < want && before + n0 + n1 >= want) { found[0] = 2046 - 2 * tid; found[1] = before + n0; }
+            __syncthreads();
+            bin = found[0];
+            over = found[1];
+            const uint32_t top = 2047 - 2 * tid;
+            // (not the last launch: this chunk's keys above the bin; the last: those of the chunks before, and ties)
+            uint32_t up = last ? (top > bin ? b0 : 0u) + (top - 1 > bin ? b1 : 0u) : (top > bin ? o0 : 0u) + (top - 1 > bin ? o1 : 0u);
+            uint32_t eq = (top == bin ? b0 : 0u) + (top - 1 == bin ? b1 : 0u);
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                up += __shfl_xor(up, o, 64);
+                eq += __shfl_xor(eq, o, 64);
+            }
+            if (lane == 0) { wsum[wave] = up; wtie[wave] = eq; }   // (every wave has read found: the sync below)
+            __syncthreads();
+            up = eq = 0;
+#pragma unroll
+            for (int i = 0; i < kSelWaves; ++i) { up += wsum[i]; eq += wtie[i]; }
+            if (last) {
+                pos += up;
+                tie = eq;
+            } else if (tid == 0) {
+                counts[((size_t)d * rows + row) * chunks + chunk] = up;
+                if (chunk == 0) reinterpret_cast<uint2*>(state)[(size_t)d * rows + row] = make_uint2(bin, over);
+            }
+        }
+        T |= bin << shift;
+        mask |= ((1u << bits) - 1) << shift;
+        need -= (int)over;
+    }
+    if (!last) {
+#pragma unroll
+        for (int i = 0; i < COPIES * kBins / kSelThreads; ++i) (&hist[0][0])[i * kSelThreads + tid] = 0;
+        __syncthreads();
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+#pragma unroll
+        for (int i = 0; i < kChunkKeys; ++i)
+            if (in[i] && (u[i] & mask) == T) atomicAdd(&hist[lane % COPIES][(u[i] >> shift) & ((1u << bits) - 1)], 1u);
+        __syncthreads();
+        uint32_t* h = a.ws + ((size_t)digit * gridDim.x + blockIdx.x) * kBins;
+#pragma unroll
+        for (int i = 0; i < kBins; i += kSelThreads) h[i + tid] = hist[0][i + tid] + hist[1][i + tid] + hist[2][i + tid] + hist[3][i + tid];
+        return;
+    }
+    // this chunk's waves before this one
+    uint32_t mine = 0, eq = 0;
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) {
+        mine += __builtin_popcountll(__ballot(in[i] && u[i] > T));
+        eq += __builtin_popcountll(__ballot(in[i] && u[i] == T));
+    }
+    __syncthreads();
+    if (lane == 0) { wsum[wave] = mine; wtie[wave] = eq; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSelWaves; ++i) {
+        pos += i < wave ? wsum[i] : 0u;
+        tie += i < wave ? wtie[i] : 0u;
+    }
+    const uint64_t lower = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; i += 4) {
+        uint32_t up = pos, at = tie;                         // before this lane's four keys
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t ba = __ballot(in[i + e] && u[i + e] > T), bt = __ballot(in[i + e] && u[i + e] == T);
+            up += __builtin_popcountll(ba & lower);
+            at += __builtin_popcountll(bt & lower);
+            pos += __builtin_popcountll(ba);
+            tie += __builtin_popcountll(bt);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = u[i + e];
+            if (!in[i + e]) continue;
+            if (x > T || (x == T && at < (uint32_t)need)) keep[up + min(at, (uint32_t)need)] = j0 + 256 * (i >> 2) + 4 * lane + e;
+            up += x > T;
+            at += x == T;
+        }
+    }
+}
+
 // ---------------------------------------------------------------- compaction
 // Key j of a (sequence, KV head) becomes key keep[j], in place.  keep ascends, so
 // keep[j] >= j: chunk by chunk a workgroup reads the sources of a run of places,
@@ -454,7 +624,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // A workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time, the
 // next chunk's loads under way while a chunk is written.  (Places past the last one
 // read its source again: loads without branches go out together.)
-template <int THREADS, int SEG, int U = 8>
+// NEAR: only the places whose source lies among the m places (a leading run, since
+// sources ascend); the others depend on no order (move_far_keys).
+template <int THREADS, int SEG, bool NEAR, int U = 8>
 __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t* keep, int m, int P) {
     constexpr int LPR = SEG / 16, STEP = THREADS / LPR;      // lanes a key, keys a pass (U of them a chunk)
     const int tid = threadIdx.x, key = tid / LPR, at = tid % LPR * 16;
@@ -473,6 +645,7 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
     load();
     indices(U * STEP);
     for (int j0 = 0; j0 < m; j0 += U * STEP) {
+        if (NEAR && keep[j0] >= m) break;
         u32x4 y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) y[u] = x[u];
@@ -485,9 +658,27 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * STEP + key;
-            if (j < m) *reinterpret_cast<u32x4*>(k + (size_t)j * row_bytes + at) = y[u];
+            if (j < m && (!NEAR || keep[j] < m)) *reinterpret_cast<u32x4*>(k + (size_t)j * row_bytes + at) = y[u];
         }
     }
+}
+
+// The places whose source lies behind the m places: nothing that is written is read
+// any more once the others have moved, so every workgroup takes places of its own.
+template <int THREADS, int U>
+__device__ __forceinline__ void move_far_keys(char* k, int row_bytes, const int32_t* keep, int m, int P, int j0) {
+    const int lpr = row_bytes / 16, step = THREADS / lpr, at = threadIdx.x % lpr * 16;
+    u32x4 x[U];
+    bool far[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int j = j0 + u * step + (int)threadIdx.x / lpr, src = keep[min(j, m - 1)];
+        far[u] = j < m && src >= m;
+        x[u] = *reinterpret_cast<const u32x4*>(k + (size_t)min(max(src, 0), P - 1) * row_bytes + at);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (far[u]) *reinterpret_cast<u32x4*>(k + (size_t)(j0 + u * step + threadIdx.x / lpr) * row_bytes + at) = x[u];
 }
 
 // A workgroup owns ROWS rows of `cap` elements; a thread takes the elements of 4
@@ -502,27 +693,46 @@ template <typename T, int THREADS, int ROWS, int E>
 __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, int m, int P) {
     constexpr int SU = 4 / sizeof(T), CHUNK = THREADS * SU * E;
     const int tid = threadIdx.x;
+    if (m < 1) return;
+    T x[ROWS][E][SU];
+    int src[E][SU];
+    auto indices = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < SU; ++i) src[e][i] = min(max(keep[min(j0 + (e * THREADS + tid) * SU + i, m - 1)], 0), P - 1);
+    };
+    auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < SU; ++i)
+#pragma unroll
+                for (int d = 0; d < ROWS; ++d) x[d][e][i] = v[(size_t)d * cap + src[e][i]];
+    };
+    indices(0);
+    load();
+    indices(CHUNK);
     for (int j0 = 0; j0 < m; j0 += CHUNK) {
-        uint32_t x[ROWS][E];
+        uint32_t y[ROWS][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            int src[SU];
+        for (int d = 0; d < ROWS; ++d)
 #pragma unroll
-            for (int i = 0; i < SU; ++i) src[i] = min(max(keep[min(j0 + (e * THREADS + tid) * SU + i, m - 1)], 0), P - 1);
-#pragma unroll
-            for (int d = 0; d < ROWS; ++d) {
-                const T* row = v + (size_t)d * cap;
+            for (int e = 0; e < E; ++e) {
                 if constexpr (SU == 1) {
-                    x[d][e] = __float_as_uint(row[src[0]]);
+                    y[d][e] = __float_as_uint(x[d][e][0]);
                 } else {
-                    x[d][e] = 0;
+                    y[d][e] = 0;
 #pragma unroll
-                    for (int i = 0; i < SU; ++i) x[d][e] |= (uint32_t)row[src[i]] << (8 * (int)sizeof(T) * i);
+                    for (int i = 0; i < SU; ++i) y[d][e] |= (uint32_t)x[d][e][i] << (8 * (int)sizeof(T) * i);
                 }
             }
-        }
-        __builtin_amdgcn_s_waitcnt(0);                       // (every source of the chunk is in registers)
-        __syncthreads();
+        // every source of the chunk is in registers; the last chunk's stores, or the first
+        // indices, which are newer, may still be under way
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(E * (SU < ROWS ? SU : ROWS)));
+        wg_barrier();
+        if (j0 + CHUNK < m) load();
+        indices(j0 + 2 * CHUNK);
 #pragma unroll
         for (int d = 0; d < ROWS; ++d)
 #pragma unroll
@@ -530,12 +740,12 @@ __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, 
                 const int j = j0 + (e * THREADS + tid) * SU;
                 T* to = v + (size_t)d * cap + j;
                 if (j + SU <= m) {
-                    *reinterpret_cast<typename Word<T>::type*>(to) = x[d][e];
+                    *reinterpret_cast<typename Word<T>::type*>(to) = y[d][e];
                 } else {
                     if constexpr (SU > 1) {
 #pragma unroll
                         for (int i = 0; i < SU; ++i)
-                            if (j + i < m) to[i] = (T)(x[d][e] >> (8 * (int)sizeof(T) * i));
+                            if (j + i < m) to[i] = (T)(y[d][e] >> (8 * (int)sizeof(T) * i));
                     }
                 }
             }
@@ -545,7 +755,7 @@ __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, 
 // Grid: the parts of every (sequence, KV head), dealt to the XCDs like the key weights'
 // units, so that segments of one line meet in one L2: segments of K's rows, groups of
 // V's rows, then (with sums) one part for them.
-template <typename T, int DH, int THREADS, int SEG, int ROWS, int E>
+template <typename T, int DH, int THREADS, int SEG, int ROWS, int E, bool NEAR>
 __global__ __launch_bounds__(THREADS) void kv_compact_kernel(KvCompactArgs a) {
     constexpr int KP = DH * (int)sizeof(T) / SEG, VP = DH / ROWS;
     const int parts = KP + VP + (a.weights ? 1 : 0), heads = a.b * a.Hkv, per = heads >> 3;
@@ -557,7 +767,7 @@ __global__ __launch_bounds__(THREADS) void kv_compact_kernel(KvCompactArgs a) {
     const size_t base = (size_t)head * a.cap * DH;
     int part = bid % parts;
     if (part < KP) {
-        move_keys<THREADS, SEG>(reinterpret_cast<char*>(a.k) + base * sizeof(T) + part * SEG, DH * sizeof(T), keep, m, p);
+        move_keys<THREADS, SEG, NEAR>(reinterpret_cast<char*>(a.k) + base * sizeof(T) + part * SEG, DH * sizeof(T), keep, m, p);
         return;
     }
     part -= KP;
@@ -566,9 +776,24 @@ __global__ __launch_bounds__(THREADS) void kv_compact_kernel(KvCompactArgs a) {
         return;
     }
     float* w = a.weights + (size_t)head * a.ldw;
-    move_values<float, THREADS, 1, 4>(w, 0, keep, m, p);
+    move_values<float, THREADS, 1, THREADS == 1024 ? 32 : 4>(w, 0, keep, m, p);   // (one workgroup a head: many at a time)
     __syncthreads();
-    for (int j = m + threadIdx.x; j < p; j += THREADS) w[j] = 0.f;   // freed places start from nothing
+    for (int j = m + 4 * (int)threadIdx.x; j < p; j += 4 * THREADS) {            // freed places start from nothing
+        if (j + 4 <= p) st_f4(w + j, floatx4{0.f, 0.f, 0.f, 0.f});
+        else
+            for (int e = j; e < p; ++e) w[e] = 0.f;
+    }
+}
+
+constexpr int kFarThreads = 256, kFarPasses = 4;
+
+template <typename T, int DH>
+__global__ __launch_bounds__(kFarThreads) void kv_compact_far_kernel(KvCompactArgs a, int blocks) {
+    constexpr int ROW = DH * (int)sizeof(T);
+    const int head = blockIdx.x / blocks, s = head / a.Hkv, p = prefix_len(a.prefix, s, a.P);
+    const int m = min(a.kept ? max(a.kept[s], 0) : a.n, min(a.n, p)), j0 = blockIdx.x % blocks * (kFarThreads / (ROW / 16) * kFarPasses);
+    if (j0 >= m) return;
+    move_far_keys<kFarThreads, kFarPasses>(reinterpret_cast<char*>(a.k) + (size_t)head * a.cap * ROW, ROW, a.keep + (size_t)head * a.n, m, p, j0);
 }
 
 }  // namespace
@@ -596,26 +821,53 @@ hipError_t launch_key_weights(int dtype, const KeyWeightArgs& a, hipStream_t s) 
     return hipGetLastError();
 }
 
+// Chunks of a row where it is long and the rows alone do not fill the chip; else 1.
+static int select_chunks(int b, int Hkv, int P) {
+    return P > kChunk && (long)b * Hkv <= 128 ? (P - 1) / kChunk + 1 : 1;
+}
+
+size_t kv_select_workspace(int b, int Hkv, int P) {
+    const int chunks = select_chunks(b, Hkv, P);
+    return chunks > 1 ? ((size_t)3 * b * Hkv * chunks * kBins + (size_t)b * Hkv * (6 + 2 * chunks)) * 4 : 0;
+}
+
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s) {
+    const int chunks = select_chunks(a.b, a.Hkv, a.P);
+    if (chunks > 1) {
+        for (int digit = 0; digit <= 3; ++digit) {
+            launch(kv_select_long_kernel, dim3((unsigned)((long)a.b * a.Hkv * chunks)), dim3(kSelThreads), 0, s, a, chunks, digit);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     const dim3 grid(a.b * a.Hkv);
-    // (a wave's run is whole 256s: up to kHeld * 64 keys of it are held)
-    if ((a.P + kSelWaves - 1) / kSelWaves <= kHeld * 64) launch(kv_select_kernel<true>, grid, dim3(kSelThreads), 0, s, a);
-    else launch(kv_select_kernel<false>, grid, dim3(kSelThreads), 0, s, a);
+    if (a.P <= 8 * kSelThreads) launch(kv_select_kernel<8>, grid, dim3(kSelThreads), 0, s, a);
+    else if (a.P <= 16 * kSelThreads) launch(kv_select_kernel<16>, grid, dim3(kSelThreads), 0, s, a);
+    else launch(kv_select_kernel<0>, grid, dim3(kSelThreads), 0, s, a);
     return hipGetLastError();
 }
 
-template <typename T, int DH, int THREADS, int SEG, int ROWS, int E>
+template <typename T, int DH, int THREADS, int SEG, int ROWS, int E, bool NEAR>
 static hipError_t compact_as(const KvCompactArgs& a, hipStream_t s) {
     const int parts = DH * (int)sizeof(T) / SEG + DH / ROWS + (a.weights ? 1 : 0);
-    launch(kv_compact_kernel<T, DH, THREADS, SEG, ROWS, E>, dim3((unsigned)((long)parts * a.b * a.Hkv)), dim3(THREADS), 0, s, a);
+    launch(kv_compact_kernel<T, DH, THREADS, SEG, ROWS, E, NEAR>, dim3((unsigned)((long)parts * a.b * a.Hkv)), dim3(THREADS), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !NEAR) return e;
+    const int per = kFarThreads / (DH * (int)sizeof(T) / 16) * kFarPasses, blocks = (a.n + per - 1) / per;
+    launch(kv_compact_far_kernel<T, DH>, dim3((unsigned)((long)blocks * a.b * a.Hkv)), dim3(kFarThreads), 0, s, a, blocks);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t compact(const KvCompactArgs& a, hipStream_t s) {
-    const bool few = (long)a.b * a.Hkv * a.dh < 4096 && a.n > 2048;
-    if (few) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 2, 2>(a, s) : compact_as<T, 64, 1024, 32, 2, 2>(a, s);
-    return a.dh == 128 ? compact_as<T, 128, 256, 64, 8, 1>(a, s) : compact_as<T, 64, 256, 64, 8, 1>(a, s);
+    // Few heads: more threads and smaller parts, and from 16384 keys on K in two launches (4 heads x 128,
+    // from memory: 131072 -> 32768 keys 155 us in 256 threads, 125 in 1024, 74 in two launches; 16384 ->
+    // 8192: 42, 32 and 35; 8192 -> 3000, twice as many heads: 21, 21 and 24).
+    const bool few = (long)a.b * a.Hkv * a.dh < 4096;
+    if (few && a.n > 16384) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 4, 2, true>(a, s) : compact_as<T, 64, 1024, 32, 4, 2, true>(a, s);
+    if (few && a.n > 4096) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 2, 2, false>(a, s) : compact_as<T, 64, 1024, 32, 2, 2, false>(a, s);
+    return a.dh == 128 ? compact_as<T, 128, 256, 64, 8, 1, false>(a, s) : compact_as<T, 64, 256, 64, 8, 1, false>(a, s);
 }
 
 hipError_t launch_kv_compact(int dtype, const KvCompactArgs& a, hipStream_t s) {

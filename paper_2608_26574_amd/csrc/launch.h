@@ -98,7 +98,9 @@ struct KvSelectArgs {
     const int32_t* prefix;
     int32_t* keep; int32_t* kept;         // [b][Hkv][n], [b] or NULL
     int b, Hkv, P, n, first, last;
+    uint32_t* ws;                         // histograms of long rows (kv_select_workspace)
 };
+size_t kv_select_workspace(int b, int Hkv, int P);
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s);
 struct KvCompactArgs {
     void* k; void* v;                     // [b][Hkv][cap][dh], [b][Hkv][dh][cap]

@@ -87,9 +87,17 @@ def select(**kw):
 @pytest.mark.parametrize("status,kw", [
     (-1, dict(w=None)), (-1, dict(keep=None)), (-1, dict(w=ODD)), (-1, dict(keep=ODD)), (-1, dict(kept=ODD)), (-1, dict(prefix=ODD)),
     (-2, dict(b=0)), (-2, dict(H=0)), (-2, dict(n=0)), (-2, dict(P=-1)), (-2, dict(ldw=99)), (-2, dict(first=-1)),
-    (-2, dict(last=-1)), (-2, dict(first=48)), (-2, dict(first=2 ** 31 - 1, last=2 ** 31 - 1)), (-2, dict(b=2 ** 30))])
+    (-2, dict(last=-1)), (-2, dict(first=48)), (-2, dict(first=2 ** 31 - 1, last=2 ** 31 - 1)), (-2, dict(b=2 ** 30)),
+    (-5, dict(P=100000, ldw=100000, ws=None)), (-5, dict(P=100000, ldw=100000, room=99)), (-1, dict(P=100000, ldw=100000, ws=ODD))])
 def test_select_refusals(status, kw):
     assert select(**kw) == status and dard.lib().dard_last_error()
+
+
+def test_select_workspace():
+    f = dard.lib().dard_kv_select_workspace_bytes
+    assert f(1, 4, 16384, 100) == 0 and f(0, 4, 100000, 100) == 0 and f(1, 4, -1, 100) == 0 and f(1, 4, 100000, 0) == 0
+    assert f(1, 4, 131072, 100) == 3 * 4 * 8 * 2048 * 4 + 4 * (6 + 16) * 4   # three digits, eight chunks of 16384 keys
+    assert f(16, 32, 131072, 100) == 0                               # rows enough: a workgroup each
 
 
 def compact(**kw):
