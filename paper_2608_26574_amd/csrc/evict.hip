@@ -15,6 +15,7 @@ namespace dard {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int prefix_len(const int32_t* prefix, int s, int P) {
     return prefix ? min(max(prefix[s], 0), P) : P;
@@ -75,7 +76,8 @@ __device__ __forceinline__ float half_sums(const float (&x)[16], int lr) {
 }
 
 template <int DH, int KB, bool KV8>
-__global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int nsplit) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(KB == 1 ? 4 : 2)))
+void key_weights_kernel(KeyWeightArgs a, int nsplit) {
     constexpr int NC = DH / 16, CH = DH / 8;                 // MFMA steps; 16-byte chunks of a row
     constexpr int STAGE = kWRows * DH * 2, NI = kWRows * CH / 256, HALVES = kWRows / 32;
     __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
@@ -164,29 +166,44 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
             bias[h] = -L[h] * kLog2e;
         }
         if (t + 1 < t1) issue(t + 1, smem + ((t + 1 - t0) & 1) * STAGE);
+        // products of PART halves of the stage in turn, then their exponentials
+        constexpr int PART = KB == 2 ? HALVES : 1;
 #pragma unroll
-        for (int half = 0; half < HALVES; ++half) {
-            bf16x8 qf[NC];
-            const int r = 32 * half + lr;
+        for (int h0 = 0; h0 < HALVES; h0 += PART) {
+            floatx16 sc[PART][KB];
+            bool all = true;
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                qf[c] = *reinterpret_cast<const bf16x8*>(cur + 16 * (r * CH + (ch(c) ^ swz(r))));
-            const bool all = __all(live[half]);
+            for (int h = 0; h < PART; ++h) {
+                bf16x8 qf[NC];
+                const int r = 32 * (h0 + h) + lr;
+                all = all && __all(live[h0 + h]);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                floatx16 sc;
+                for (int c = 0; c < NC; ++c)
+                    qf[c] = *reinterpret_cast<const bf16x8*>(cur + 16 * (r * CH + (ch(c) ^ swz(r))));
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sc[v] = 0.f;
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int c = 0; c < NC; ++c) sc = mfma32x32x16(kf[kb][c], qf[c], sc);
-                if (all) {
+                    for (int v = 0; v < 16; ++v) sc[h][kb][v] = 0.f;
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) acc[kb][v] += __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias[half]));
-                } else {
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        acc[kb][v] += live[half] ? __builtin_amdgcn_exp2f(fmaf(sc[v], sl2, bias[half])) : 0.f;
-                }
+                    for (int kb = 0; kb < KB; ++kb) sc[h][kb] = mfma32x32x16(kf[kb][c], qf[c], sc[h][kb]);
+            }
+            if (all) {
+#pragma unroll
+                for (int h = 0; h < PART; ++h)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) acc[kb][v] += __builtin_amdgcn_exp2f(fmaf(sc[h][kb][v], sl2, bias[h0 + h]));
+            } else {
+#pragma unroll
+                for (int h = 0; h < PART; ++h)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            acc[kb][v] += live[h0 + h] ? __builtin_amdgcn_exp2f(fmaf(sc[h][kb][v], sl2, bias[h0 + h])) : 0.f;
             }
         }
     }
@@ -199,6 +216,101 @@ __global__ __launch_bounds__(256) void key_weights_kernel(KeyWeightArgs a, int n
             if (nsplit > 1) a.part[((size_t)split * a.b * a.Hkv + un.head) * a.P + key] = x;
             else a.weights[(size_t)un.head * a.ldw + key] = fmaf(a.decay, old[kb], x);
         }
+    }
+}
+
+// Few rows (up to 32 HB): the rows stay in a wave's registers and its keys stream
+// through them, a block of 32 ahead of the one at work; no LDS, no barrier.  S = Q K^T,
+// so a lane holds 16 rows' scores of one key and adds them by itself.
+template <int DH, int HB, bool KV8>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void key_weights_few_kernel(KeyWeightArgs a, int blocks) {
+    constexpr int NC = DH / 16, NL = KV8 ? NC / 2 : NC;      // MFMA steps; 16-byte loads of a lane
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lr = lane & 31, eta = lane >> 5;
+    const WeightUnit un = weight_unit(a, 1, 128 * blocks);   // (a wave takes `blocks` blocks in a row)
+    const int g = un.head % a.Hkv, s = un.head / a.Hkv;
+    const int p = prefix_len(a.prefix, s, a.P), k0 = (un.kt * 4 + wave) * 32 * blocks, k1 = min(p, k0 + 32 * blocks);
+    if (k0 >= k1) return;
+    const int GQ = a.Hq / a.Hkv, rows = GQ * a.R;
+    auto ch = [&](int c) __attribute__((always_inline)) { return 4 * (c >> 1) + 2 * eta + (c & 1); };   // (as above)
+    const char* kb = reinterpret_cast<const char*>(a.k) + ((size_t)s * a.Hkv + g) * a.cap * DH * (KV8 ? 1 : 2);
+    float* w = a.weights + (size_t)un.head * a.ldw;
+    u32x4 next[NL];
+    float old;
+    auto fetch = [&](int k) __attribute__((always_inline)) {
+        const int key = min(k + lr, p - 1);
+#pragma unroll
+        for (int c = 0; c < NL; ++c)
+            next[c] = KV8 ? *reinterpret_cast<const u32x4*>(kb + (size_t)key * DH + 8 * ch(2 * c))
+                          : *reinterpret_cast<const u32x4*>(kb + ((size_t)key * DH + 8 * ch(c)) * 2);
+        old = a.decay != 0.f ? w[key] : 0.f;
+    };
+    fetch(k0);
+    // the rows: A operand row lr of block h, and -L of the 16 rows whose scores the lane holds
+    bf16x8 qf[HB][NC];
+    float bias[HB][16];
+    uint32_t live = 0;                                       // bit 16 h + v (a row without a sum counts nothing)
+    const size_t base = (size_t)s * a.R * a.Hq + (size_t)g * GQ;
+#pragma unroll
+    for (int h = 0; h < HB; ++h) {
+        const int rho = min(32 * h + lr, rows - 1);
+        const bf16_t* q = reinterpret_cast<const bf16_t*>(a.q) + (base + (size_t)(rho / GQ) * a.Hq + rho % GQ) * DH;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) qf[h][c] = ld_bf16x8(q + 8 * ch(c));
+        const float mine = 32 * h + lr < rows ? a.lse[base + (size_t)(rho / GQ) * a.Hq + rho % GQ] : INFINITY;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const float L = __shfl(mine, 8 * (v >> 2) + 4 * eta + (v & 3), 64);
+            bias[h][v] = -L * kLog2e;
+            if (fabsf(L) < INFINITY || L != L) live |= 1u << (16 * h + v);
+        }
+    }
+    const bool all = __all(live == (HB == 2 ? 0xFFFFFFFFu : 0xFFFFu));
+    const float sl2 = a.scale * kLog2e;
+    for (int k = k0; k < k1; k += 32) {
+        bf16x8 kf[NC];
+#pragma unroll
+        for (int c = 0; c < NL; ++c) {
+            if constexpr (KV8) {
+                kf[2 * c] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8_scaled(next[c][0], next[c][1]));
+                kf[2 * c + 1] = __builtin_bit_cast(bf16x8, e4m3x8_to_bf16x8_scaled(next[c][2], next[c][3]));
+            } else {
+                kf[c] = __builtin_bit_cast(bf16x8, next[c]);
+            }
+        }
+        const float was = old;
+        if (k + 32 < k1) fetch(k + 32);
+        floatx16 sc[HB];
+#pragma unroll
+        for (int h = 0; h < HB; ++h)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[h][v] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int h = 0; h < HB; ++h) sc[h] = mfma32x32x16(qf[h][c], kf[c], sc[h]);
+        float x = 0.f, y = 0.f;
+        if (all) {
+#pragma unroll
+            for (int h = 0; h < HB; ++h)
+#pragma unroll
+                for (int v = 0; v < 16; v += 2) {
+                    x += __builtin_amdgcn_exp2f(fmaf(sc[h][v], sl2, bias[h][v]));
+                    y += __builtin_amdgcn_exp2f(fmaf(sc[h][v + 1], sl2, bias[h][v + 1]));
+                }
+        } else {
+#pragma unroll
+            for (int h = 0; h < HB; ++h)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(sc[h][v], sl2, bias[h][v]));
+                    x += (live >> (16 * h + v)) & 1u ? e : 0.f;
+                }
+        }
+        x += y;
+        x += __shfl_xor(x, 32, 64);
+        if (eta == 0 && k + lr < k1) w[k + lr] = fmaf(a.decay, was, x);
     }
 }
 
@@ -271,12 +383,25 @@ __global__ __launch_bounds__(256) void key_weights_sum_kernel(KeyWeightArgs a, i
 }
 
 struct WeightCfg {
+    int few;          // rows in registers: blocks of 32 rows, else 0
     int kb, ktiles, ns;
 };
 
 WeightCfg weight_cfg(int dtype, int b, int R, int Hq, int Hkv, int P) {
     WeightCfg c{};
     const long rows = (long)R * (Hq / Hkv), heads = (long)b * Hkv;
+    // Few rows stay in registers where the keys are enough for 8 waves a CU (kb: blocks of
+    // 32 that a wave takes in a row): 64 rows of 16 x 32 heads, FP8, up to 1664 keys 22 us
+    // (rows in LDS: 28), 8 rows of 8 x 32 heads over 4096 keys 44 (56); 64 rows of 32 heads
+    // over 609 keys 6.3 (5.3).
+    const long blocks = heads * ((P + 31) / 32);
+    if (dtype != DARD_DTYPE_F32 && rows <= 64 && blocks >= 2048) {
+        c.few = rows > 32 ? 2 : 1;
+        c.kb = (int)std::min<long>(16, blocks / 2048);
+        c.ktiles = (P + 128 * c.kb - 1) / (128 * c.kb);
+        c.ns = 1;
+        return c;
+    }
     c.kb = dtype == DARD_DTYPE_F32 || rows < 512 || heads * ((P + 255) / 256) < 256 ? 1 : 2;
     c.ktiles = (P + 128 * c.kb - 1) / (128 * c.kb);
     const long wgs = heads * c.ktiles, tiles = (rows + kWRows - 1) / kWRows;
@@ -619,8 +744,6 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArg
 // then writes that run, which no later chunk reads.  A workgroup owns whole
 // columns (a run of a key's bytes, or rows of the dims-major V), so the order of
 // reads and writes is its own affair.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 // A workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time, the
 // next chunk's loads under way while a chunk is written.  (Places past the last one
 // read its source again: loads without branches go out together.)
@@ -807,6 +930,15 @@ hipError_t launch_key_weights(int dtype, const KeyWeightArgs& a, hipStream_t s) 
     const WeightCfg c = weight_cfg(dtype, a.b, a.R, a.Hq, a.Hkv, a.P);
     const dim3 grid((unsigned)((long)a.b * a.Hkv * c.ktiles * c.ns));
     void (*k)(KeyWeightArgs, int);
+    if (c.few) {
+        const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8, two = c.few == 2;
+        if (a.dh == 128) k = kv8 ? (two ? key_weights_few_kernel<128, 2, true> : key_weights_few_kernel<128, 1, true>)
+                                 : (two ? key_weights_few_kernel<128, 2, false> : key_weights_few_kernel<128, 1, false>);
+        else k = kv8 ? (two ? key_weights_few_kernel<64, 2, true> : key_weights_few_kernel<64, 1, true>)
+                     : (two ? key_weights_few_kernel<64, 2, false> : key_weights_few_kernel<64, 1, false>);
+        launch(k, dim3((unsigned)((long)a.b * a.Hkv * c.ktiles)), dim3(256), 0, s, a, c.kb);
+        return hipGetLastError();
+    }
     if (dtype == DARD_DTYPE_F32) k = a.dh == 128 ? key_weights_f32_kernel<128> : key_weights_f32_kernel<64>;
     else if (dtype == DARD_DTYPE_BF16_KV_FP8)
         k = a.dh == 128 ? (c.kb == 2 ? key_weights_kernel<128, 2, true> : key_weights_kernel<128, 1, true>)

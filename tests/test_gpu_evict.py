@@ -53,7 +53,8 @@ def weights_case(dtype, b, R, P, Hq, Hkv, dh, lens=None, decay=0.9, seed=0, extr
 @pytest.mark.parametrize("dtype", [E.BF16, E.FP8, E.F32])
 @pytest.mark.parametrize("b,R,P,Hq,Hkv,dh", [
     (1, 1, 1, 1, 1, 64), (1, 1, 300, 4, 4, 128), (2, 3, 33, 4, 2, 64), (1, 64, 609, 4, 4, 128), (3, 31, 130, 14, 2, 128),
-    (1, 200, 40, 7, 1, 128), (2, 65, 257, 3, 3, 64), (5, 2, 700, 28, 4, 128), (40, 5, 300, 16, 16, 64), (1, 700, 3, 28, 4, 64)])
+    (1, 200, 40, 7, 1, 128), (2, 65, 257, 3, 3, 64), (5, 2, 700, 28, 4, 128), (40, 5, 300, 16, 16, 64), (1, 700, 3, 28, 4, 64),
+    (33, 7, 2000, 4, 1, 128), (20, 6, 3500, 14, 2, 64), (40, 61, 2100, 1, 1, 128)])
 def test_key_weights(dtype, b, R, P, Hq, Hkv, dh):
     announce("key weights", dtype, b, R, P, Hq, Hkv, dh)
     weights_case(dtype, b, R, P, Hq, Hkv, dh)
@@ -67,6 +68,16 @@ def test_key_weights_ragged_rows_without_sum_and_old_sums(dtype):
     weights_case(dtype, 1, 400, 60, 14, 2, 64, dead=True, seed=3)
     weights_case(dtype, 2, 9, 64, 2, 2, 64, decay=0.0, old=float("nan"), seed=4)      # decay 0 does not read them
     weights_case(dtype, 2, 300, 64, 2, 2, 64, decay=0.0, old=float("inf"), seed=5)
+
+
+@pytest.mark.parametrize("dtype", [E.BF16, E.FP8])
+def test_key_weights_of_few_rows(dtype):
+    """Few rows over many keys (rows in registers): lengths of their own, rows without a sum, sums further apart."""
+    announce("key weights few rows", dtype)
+    lens = [(97 * i) % 2101 for i in range(34)]
+    weights_case(dtype, 34, 13, 2100, 2, 2, 128, lens=lens, decay=1.0, seed=6)
+    weights_case(dtype, 34, 32, 2100, 4, 2, 64, lens=lens, dead=True, seed=7)
+    weights_case(dtype, 34, 64, 2100, 2, 2, 64, decay=0.0, old=float("nan"), seed=8)
 
 
 def test_key_weights_of_a_shared_cache_and_strided_sums():
@@ -100,6 +111,32 @@ def test_key_weights_of_broken_keys_and_rows():
     q[0, 2, 3, 0] = float("nan")
     dard.dard_key_weights(q, lse, k, 80, 0.125, 0.0, w)
     assert torch.isnan(w[0, 1]).all() and torch.isnan(w[0, 0]).sum() == 1
+    lse[0, 2, 3] = float("inf")   # the row counts nothing, whatever it holds
+    dard.dard_key_weights(q, lse, k, 80, 0.125, 0.0, w)
+    assert torch.isnan(w).sum() == 1
+
+
+def test_key_weights_of_broken_keys_and_few_rows():
+    """The same where the rows stay in registers."""
+    announce("key weights NaN, few rows")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k = torch.randn(40, 5, 2, 64, generator=g, device="cuda").bfloat16(), torch.randn(40, 2, 1000, 64, generator=g, device="cuda").bfloat16()
+    lse, w0 = torch.full((40, 5, 2), 5.0, device="cuda"), torch.zeros(40, 2, 1000, device="cuda")
+    dard.dard_key_weights(q, lse, k, 1000, 0.125, 0.0, w0)
+    k[3, 0, 7, 3], q[2, 1, 1, 0], q[1, 2, 0, 0], lse[1, 2, 0] = float("nan"), float("nan"), float("nan"), float("inf")
+    lse2 = lse.clone()
+    lse2[1, 2, 0] = 5.0
+    w, clean = torch.zeros_like(w0), q.clone()
+    clean[1, 2, 0, 0] = 0.0
+    dard.dard_key_weights(q, lse, k, 1000, 0.125, 0.0, w)
+    bad = torch.zeros_like(w, dtype=torch.bool)
+    bad[3, 0, 7], bad[2, 1] = True, True
+    assert torch.equal(torch.isnan(w), bad)
+    rest = ~bad
+    rest[1, 0] = False
+    assert torch.equal(w[rest], w0[rest])
+    ref = torch.exp(clean[1].float().transpose(0, 1) @ k[1].float().transpose(-1, -2) * 0.125 - 5.0)[0]
+    assert torch.all((w[1, 0] - ref[[0, 1, 3, 4]].sum(0)).abs() <= 2.0 ** -14 * ref.sum(0))
 
 
 # ------------------------------------------------------------------ selection
