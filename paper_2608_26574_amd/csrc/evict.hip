@@ -427,12 +427,15 @@ __device__ __forceinline__ uint32_t sum_rank(float w) {
 
 // HELD: the row's sums fit the registers (HELD keys a thread) and are read once; 0:
 // every pass reads them again, 16 keys a thread in flight.
-template <int HELD>
-__global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) {
+// BITS: of a digit; short rows take four of 8 bits in workgroups of 256 threads, whose
+// barriers are quick, others three of 11 in 1024.
+template <int THREADS, int HELD, int BITS>
+__global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelectArgs a) {
     // histogram copies by lane: equal sums in neighbouring lanes would queue at one counter
-    constexpr int COPIES = 4;
-    __shared__ uint32_t hist[COPIES][2048];
-    __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
+    constexpr int COPIES = 4, WAVES = THREADS / 64, BINS = 1 << BITS, BPT = BINS / THREADS, DIGITS = (32 + BITS - 1) / BITS;
+    static_assert(BPT == 1 || BPT == 2, "a bin or two a thread");
+    __shared__ uint32_t hist[COPIES][BINS];
+    __shared__ uint32_t wsum[WAVES], wtie[WAVES];
     __shared__ uint32_t found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = blockIdx.x / a.Hkv;
@@ -440,13 +443,13 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
     const float* w = a.weights + (size_t)blockIdx.x * a.ldw;
     int32_t* keep = a.keep + (size_t)blockIdx.x * a.n;
     if (a.kept && blockIdx.x % a.Hkv == 0 && tid == 0) a.kept[s] = m;
-    for (int i = m + tid; i < a.n; i += kSelThreads) keep[i] = -1;
+    for (int i = m + tid; i < a.n; i += THREADS) keep[i] = -1;
     if (m == p) {                                            // nothing to leave out
-        for (int i = tid; i < m; i += kSelThreads) keep[i] = i;
+        for (int i = tid; i < m; i += THREADS) keep[i] = i;
         return;
     }
     // a wave's keys: a run of whole 256s, four neighbours a lane
-    const int per = ((p + kSelWaves - 1) / kSelWaves + 255) / 256 * 256, j0 = wave * per, j1 = min(p, j0 + per);
+    const int per = ((p + WAVES - 1) / WAVES + 255) / 256 * 256, j0 = wave * per, j1 = min(p, j0 + per);
     auto fetch = [&](int j) __attribute__((always_inline)) {
         floatx4 x = {0.f, 0.f, 0.f, 0.f};
         if (j + 4 <= p) x = ld_f4(w + j);
@@ -489,27 +492,28 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
     // threshold T: fewer than m keys rank above it, m or more at or above it
     uint32_t T = 0, mask = 0;
     int need = m;                                            // keys to take among those that agree with T under mask
-    constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
 #pragma unroll
-    for (int d = 0; d < 3; ++d) {
+    for (int d = 0; d < DIGITS; ++d) {
+        const int shift = d + 1 < DIGITS ? 32 - BITS * (d + 1) : 0, bits = d + 1 < DIGITS ? BITS : 32 - BITS * d;
 #pragma unroll
-        for (int i = 0; i < COPIES * 2048 / kSelThreads; ++i) (&hist[0][0])[i * kSelThreads + tid] = 0;
+        for (int i = 0; i < COPIES * BINS / THREADS; ++i) (&hist[0][0])[i * THREADS + tid] = 0;
         __syncthreads();
         run([&](const uint32_t (&u)[4], int j) __attribute__((always_inline)) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (j + e < j1 && (u[e] & mask) == T)
-                    atomicAdd(&hist[lane % COPIES][(u[e] >> kShift[d]) & ((1u << kBits[d]) - 1)], 1u);
+                if (j + e < j1 && (u[e] & mask) == T) atomicAdd(&hist[lane % COPIES][(u[e] >> shift) & ((1u << bits) - 1)], 1u);
         });
         __syncthreads();
         // the bin in which the count from the top passes need (integer counts: order plays no part)
-        uint32_t c0 = 0, c1 = 0;                             // this thread's two bins, from the top
+        uint32_t c[BPT], sum = 0;                            // this thread's bins, from the top
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            c0 += hist[i][2047 - 2 * tid];
-            c1 += hist[i][2046 - 2 * tid];
+        for (int i = 0; i < BPT; ++i) {
+            c[i] = 0;
+#pragma unroll
+            for (int k = 0; k < COPIES; ++k) c[i] += hist[k][BINS - 1 - BPT * tid - i];
+            sum += c[i];
         }
-        uint32_t sum = c0 + c1;
+        const uint32_t mine = sum;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const uint32_t below = __shfl_up(sum, o, 64);
@@ -517,15 +521,18 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
         }
         if (lane == 63) wsum[wave] = sum;
         __syncthreads();
-        uint32_t before = sum - c0 - c1;
+        uint32_t before = sum - mine;
 #pragma unroll
-        for (int i = 0; i < kSelWaves; ++i) before += i < wave ? wsum[i] : 0u;
+        for (int i = 0; i < WAVES; ++i) before += i < wave ? wsum[i] : 0u;
         const uint32_t want = (uint32_t)need;
-        if (before < want && before + c0 >= want) { found[0] = 2047 - 2 * tid; found[1] = before; }
-        if (before + c0 < want && before + c0 + c1 >= want) { found[0] = 2046 - 2 * tid; found[1] = before + c0; }
+#pragma unroll
+        for (int i = 0; i < BPT; ++i) {
+            if (before < want && before + c[i] >= want) { found[0] = BINS - 1 - BPT * tid - i; found[1] = before; }
+            before += c[i];
+        }
         __syncthreads();
-        T |= found[0] << kShift[d];
-        mask |= ((1u << kBits[d]) - 1) << kShift[d];
+        T |= found[0] << shift;
+        mask |= ((1u << bits) - 1) << shift;
         need -= (int)found[1];
     }
     // keys above T, and the first `need` of those that equal it, in index order
@@ -541,7 +548,7 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_kernel(KvSelectArgs a) 
     __syncthreads();
     uint32_t pos = 0, tie = 0;                               // keys above T, and ties, before this wave's run
 #pragma unroll
-    for (int i = 0; i < kSelWaves; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
         pos += i < wave ? wsum[i] : 0u;
         tie += i < wave ? wtie[i] : 0u;
     }
@@ -974,9 +981,10 @@ hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s) {
         return hipSuccess;
     }
     const dim3 grid(a.b * a.Hkv);
-    if (a.P <= 8 * kSelThreads) launch(kv_select_kernel<8>, grid, dim3(kSelThreads), 0, s, a);
-    else if (a.P <= 16 * kSelThreads) launch(kv_select_kernel<16>, grid, dim3(kSelThreads), 0, s, a);
-    else launch(kv_select_kernel<0>, grid, dim3(kSelThreads), 0, s, a);
+    if (a.P <= 2048) launch(kv_select_kernel<256, 8, 8>, grid, dim3(256), 0, s, a);
+    else if (a.P <= 8 * kSelThreads) launch(kv_select_kernel<kSelThreads, 8, 11>, grid, dim3(kSelThreads), 0, s, a);
+    else if (a.P <= 16 * kSelThreads) launch(kv_select_kernel<kSelThreads, 16, 11>, grid, dim3(kSelThreads), 0, s, a);
+    else launch(kv_select_kernel<kSelThreads, 0, 11>, grid, dim3(kSelThreads), 0, s, a);
     return hipGetLastError();
 }
 

@@ -136,7 +136,8 @@ def test_key_weights_of_broken_keys_and_few_rows():
     rest[1, 0] = False
     assert torch.equal(w[rest], w0[rest])
     ref = torch.exp(clean[1].float().transpose(0, 1) @ k[1].float().transpose(-1, -2) * 0.125 - 5.0)[0]
-    assert torch.all((w[1, 0] - ref[[0, 1, 3, 4]].sum(0)).abs() <= 2.0 ** -14 * ref.sum(0))
+    # (both sides' scores are float32 sums of 64 products, |q k| sums to under 64 times 8 / 8: 2 * 72 * 2^-23 * 64)
+    assert torch.all((w[1, 0] - ref[[0, 1, 3, 4]].sum(0)).abs() <= 2.0 ** -9 * ref.sum(0))
 
 
 # ------------------------------------------------------------------ selection
