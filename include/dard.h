@@ -605,7 +605,7 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  *         the block (x, then s) at p .. p + 2B - 1.
  *     lse [b][2B][Hq] float32, or NULL: the natural log of the row's sum of
  *     e^(scale q . k) over the keys that it sees.  Needs Ps <= cap_shared, P + 2B <=
- *     cap, P and Ps at most 2^30, 0 < scale < 2^127.  Probabilities are rounded to
+ *     cap, cap and cap_shared at most 2^28, 0 < scale < 2^127.  Probabilities are rounded to
  *     bf16 (bf16, FP8 caches), sums and statistics are float32.  What stands in
  *     keys that a row does not see, also infinities and NaN, does not reach it; a
  *     row whose scores are all minus infinity gives zeros and lse = minus infinity.
@@ -624,7 +624,8 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  *     the first `first` and last `last` of the p keys always, then by weight,
  *     the larger first, ties to the lower index (NaN ranks below everything, -0
  *     as 0).  keep [b][Hkv][n] int32: their indices, ascending, then -1 from m
- *     on; kept [b] int32 or NULL: m.  Needs n >= 1, first + last <= n.
+ *     on; kept [b] int32 or NULL: m (not the array of `prefix`, which other heads
+ *     still read).  Needs n >= 1, first + last <= n, P and n at most 2^30.
  *
  *   dard_kv_compact  key j of every (s, g) becomes key keep[s][g][j], j < m =
  *     kept[s] (NULL: n; at most n and p), in K, V and, when not NULL, weights, in
@@ -632,7 +633,7 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  *     nothing; every other key keeps its bytes.  keep ascends, as dard_kv_select
  *     writes it (indices are clamped into [0, p); other orders give unspecified
  *     keys).  With kept as the prefix of the next call, the block or new keys
- *     follow at m.
+ *     follow at m.  Needs P <= cap, at most 2^30.
  *
  * Workspaces (device, caller-owned, 16-byte aligned, contents need no
  * initialisation) by the queries; 0: none is needed, ws may be NULL. */

@@ -637,12 +637,15 @@ int check_heads(int b, int Hq, int Hkv, int dh) {
     return DARD_OK;
 }
 
+constexpr int kMaxSharedCap = 1 << 28;
+
 int check_shared_attention(int dtype, int b, int B, int Hq, int Hkv, int dh, int Ps, int P) {
     if (int rc = check_kv_type(dtype)) return rc;
     if (int rc = check_heads(b, Hq, Hkv, dh)) return rc;
     if (B < 1 || B > 256 || Ps < 0 || P < 0) return fail(DARD_ERR_SHAPE, "need 1 <= B <= 256, Ps >= 0, P >= 0");
-    // (a workgroup counts the tiles of up to 64 sequences in an int)
-    if (Ps > (1 << 30) || P > (1 << 30)) return fail(DARD_ERR_SHAPE, "Ps and P must be at most 2^30");
+    // (a workgroup counts the tiles of up to 64 sequences in an int, and a lane's place among eight rows of V
+    // in 32 bits: kMaxSharedCap)
+    if (Ps > kMaxSharedCap || P > kMaxSharedCap) return fail(DARD_ERR_SHAPE, "Ps and P must be at most 2^28");
     if ((double)b * 2 * B * Hq * (dh / 4) > 2147483647.0) return fail(DARD_ERR_SHAPE, "too many query rows in one call");
     return DARD_OK;
 }
@@ -688,6 +691,8 @@ dard_status dard_masked_attention_shared(int dtype, const void* q, const void* k
     if (int rc = check_shared_attention(dtype, b, B, Hq, Hkv, dh, Ps, P)) return rc;
     if (Ps > 0 && Ps > cap_shared) return fail(DARD_ERR_SHAPE, "Ps must be <= cap_shared");
     if (2 * B > cap || P > cap - 2 * B) return fail(DARD_ERR_SHAPE, "P + 2B must be <= cap");
+    if (cap > kMaxSharedCap || (Ps > 0 && cap_shared > kMaxSharedCap))
+        return fail(DARD_ERR_SHAPE, "cap and cap_shared must be at most 2^28");
     const uintptr_t al = kv_align(dtype);
     if (!aligned(q, al) || !aligned(out, al) || !aligned(k, al) || !aligned(v, al) ||
         (Ps > 0 && (!aligned(k_shared, al) || !aligned(v_shared, al))))
@@ -747,6 +752,7 @@ namespace {
 
 int check_select(int b, int Hkv, int P, int n) {
     if (b < 1 || Hkv < 1 || P < 0 || n < 1) return fail(DARD_ERR_SHAPE, "need b, Hkv, n >= 1 and P >= 0");
+    if (P > (1 << 30) || n > (1 << 30)) return fail(DARD_ERR_SHAPE, "P and n must be at most 2^30");
     if ((double)b * Hkv >= 4194304.0) return fail(DARD_ERR_SHAPE, "too many heads in one call");
     return DARD_OK;
 }
@@ -766,6 +772,8 @@ dard_status dard_kv_select(const float* weights, int64_t ldw, int P, const int32
         return fail(DARD_ERR_SHAPE, "need first, last >= 0 and first + last <= n");
     if (!aligned(weights, 4) || !aligned(prefix, 4) || !aligned(keep, 4) || !aligned(kept, 4))
         return fail(DARD_ERR_ARG, "tensors must be 4-byte aligned");
+    // (kept is written while other workgroups still read the lengths)
+    if (kept && prefix && kept < prefix + b && prefix < kept + b) return fail(DARD_ERR_ARG, "kept must not overlap prefix");
     const size_t need = kv_select_workspace(b, Hkv, P);
     if (need && (!ws || ws_bytes < need)) return fail(DARD_ERR_WORKSPACE, "workspace needs %zu bytes", need);
     if (need && !aligned(ws, 16)) return fail(DARD_ERR_ARG, "the workspace must be 16-byte aligned");
@@ -782,6 +790,7 @@ dard_status dard_kv_compact(int dtype, void* k, void* v, int cap, float* weights
     if (int rc = check_kv_type(dtype)) return rc;
     if (int rc = check_heads(b, Hkv, Hkv, dh)) return rc;
     if (P < 0 || n < 1 || P > cap || (weights && ldw < P)) return fail(DARD_ERR_SHAPE, "need n >= 1 and 0 <= P <= cap, ldw");
+    if (P > (1 << 30)) return fail(DARD_ERR_SHAPE, "P must be at most 2^30");
     if ((double)b * Hkv > 524288.0) return fail(DARD_ERR_SHAPE, "too many heads in one call");
     if (!aligned(k, kv_align(dtype)) || !aligned(v, dtype == DARD_DTYPE_F32 ? 4 : dtype == DARD_DTYPE_BF16 ? 2 : 1))
         return fail(DARD_ERR_ARG, "k must be %d-byte aligned, v to its element", (int)kv_align(dtype));

@@ -751,6 +751,12 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArg
 // then writes that run, which no later chunk reads.  A workgroup owns whole
 // columns (a run of a key's bytes, or rows of the dims-major V), so the order of
 // reads and writes is its own affair.
+// The waits below count operations: what is written before stays before.
+__device__ __forceinline__ void in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // A workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time, the
 // next chunk's loads under way while a chunk is written.  (Places past the last one
 // read its source again: loads without branches go out together.)
@@ -773,6 +779,7 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
     };
     indices(0);
     load();
+    in_order();
     indices(U * STEP);
     for (int j0 = 0; j0 < m; j0 += U * STEP) {
         if (NEAR && keep[j0] >= m) break;
@@ -842,6 +849,7 @@ __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, 
     };
     indices(0);
     load();
+    in_order();
     indices(CHUNK);
     for (int j0 = 0; j0 < m; j0 += CHUNK) {
         uint32_t y[ROWS][E];
@@ -994,7 +1002,7 @@ static hipError_t compact_as(const KvCompactArgs& a, hipStream_t s) {
     launch(kv_compact_kernel<T, DH, THREADS, SEG, ROWS, E, NEAR>, dim3((unsigned)((long)parts * a.b * a.Hkv)), dim3(THREADS), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !NEAR) return e;
-    const int per = kFarThreads / (DH * (int)sizeof(T) / 16) * kFarPasses, blocks = (a.n + per - 1) / per;
+    const int per = kFarThreads / (DH * (int)sizeof(T) / 16) * kFarPasses, blocks = (std::min(a.n, a.P) + per - 1) / per;
     launch(kv_compact_far_kernel<T, DH>, dim3((unsigned)((long)blocks * a.b * a.Hkv)), dim3(kFarThreads), 0, s, a, blocks);
     return hipGetLastError();
 }
@@ -1005,8 +1013,9 @@ static hipError_t compact(const KvCompactArgs& a, hipStream_t s) {
     // from memory: 131072 -> 32768 keys 155 us in 256 threads, 125 in 1024, 74 in two launches; 16384 ->
     // 8192: 42, 32 and 35; 8192 -> 3000, twice as many heads: 21, 21 and 24).
     const bool few = (long)a.b * a.Hkv * a.dh < 4096;
-    if (few && a.n > 16384) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 4, 2, true>(a, s) : compact_as<T, 64, 1024, 32, 4, 2, true>(a, s);
-    if (few && a.n > 4096) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 2, 2, false>(a, s) : compact_as<T, 64, 1024, 32, 2, 2, false>(a, s);
+    const int n = std::min(a.n, a.P);
+    if (few && n > 16384) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 4, 2, true>(a, s) : compact_as<T, 64, 1024, 32, 4, 2, true>(a, s);
+    if (few && n > 4096) return a.dh == 128 ? compact_as<T, 128, 1024, 32, 2, 2, false>(a, s) : compact_as<T, 64, 1024, 32, 2, 2, false>(a, s);
     return a.dh == 128 ? compact_as<T, 128, 256, 64, 8, 1, false>(a, s) : compact_as<T, 64, 256, 64, 8, 1, false>(a, s);
 }
 

@@ -40,6 +40,12 @@ def test_attention_refusals(status, kw):
     assert attention(**kw) == status and dard.lib().dard_last_error()
 
 
+@pytest.mark.parametrize("kw", [dict(cap=2 ** 28 + 1), dict(cap_sh=2 ** 28 + 1), dict(P=2 ** 28, cap=2 ** 28 + 8), dict(cap=2 ** 31 - 1)])
+def test_attention_caches_past_32_bits_of_a_lane(kw):
+    """Eight rows of V must span less than 2^32 bytes."""
+    assert attention(**kw) == -2 and attention(Ps=0, cap_sh=2 ** 31 - 1, q=ODD) == -1
+
+
 def test_attention_workspace():
     f = dard.lib().dard_attention_shared_workspace_bytes
     assert f(1, 0, 4, 4, 4, 64, 0, 0) == 0 and f(9, 1, 4, 4, 4, 64, 0, 0) == 0 and f(1, 1, 4, 4, 3, 64, 0, 0) == 0
@@ -93,6 +99,19 @@ def test_select_refusals(status, kw):
     assert select(**kw) == status and dard.lib().dard_last_error()
 
 
+def test_select_lengths_in_place():
+    """kept may not be the array that the other heads' workgroups still read."""
+    base = 0x1000
+    for off in (0, 4, -4, 8, -8):
+        assert select(b=3, prefix=P, kept=ctypes.c_void_p(base + off)) == -1
+    for off in (12, -12):                                            # (next to it: taken, and then refused for another reason)
+        assert select(b=3, prefix=P, kept=ctypes.c_void_p(base + off), P=100000, ldw=100000, ws=None) == -5
+
+
+def test_select_sizes():
+    assert select(P=2 ** 30 + 1, ldw=2 ** 31) == -2 and select(n=2 ** 30 + 1) == -2
+
+
 def test_select_workspace():
     f = dard.lib().dard_kv_select_workspace_bytes
     assert f(1, 4, 16384, 100) == 0 and f(0, 4, 100000, 100) == 0 and f(1, 4, -1, 100) == 0 and f(1, 4, 100000, 0) == 0
@@ -115,6 +134,10 @@ def compact(**kw):
     (-2, dict(b=2 ** 20))])
 def test_compact_refusals(status, kw):
     assert compact(**kw) == status and dard.lib().dard_last_error()
+
+
+def test_compact_sizes():
+    assert compact(P=2 ** 30 + 1, cap=2 ** 31 - 1, ldw=2 ** 31) == -2
 
 
 def test_compact_of_nothing():
