@@ -201,6 +201,15 @@ def test_select_ragged_and_strided():
     select_case(w, 100, 4, 16, lens=[50, 99, 299, 150, 7, 300, 20], ld=333)
 
 
+@pytest.mark.parametrize("n", [1, 20000, 45000])
+def test_select_long_ragged(n):
+    """Rows of several workgroups whose lengths end at, and beside, the keys of one; more places than keys."""
+    announce("select long ragged", n)
+    rng = np.random.default_rng(n)
+    w = rng.random((7, 2, 40000)).astype(np.float32)
+    select_case(w, n, 1, 0, lens=[40000, 16384, 16385, 5, 0, 32769, 32768], ld=40003)
+
+
 # ------------------------------------------------------------------ compaction
 def compact_case(dtype, b, H, P, dh, n, extra=0, lens=None, kept=True, sums=True, seed=0):
     rng = np.random.default_rng(seed + P + n)
@@ -246,6 +255,16 @@ def test_compact_ragged_and_without_sums(dtype):
     announce("compact ragged", dtype)
     compact_case(dtype, 6, 2, 300, 64, 120, 9, lens=[0, 300, 1, -5, 777, 121], seed=1)
     compact_case(dtype, 2, 2, 700, 128, 300, 1, kept=False, sums=False, seed=2)
+
+
+@pytest.mark.parametrize("dtype", [E.BF16, E.FP8, E.F32])
+@pytest.mark.parametrize("b,H,P,dh,n,lens", [
+    (1, 2, 9000, 128, 5000, None), (1, 1, 40000, 64, 17000, None), (1, 1, 20000, 128, 19999, None), (1, 1, 20000, 64, 30000, None),
+    (4, 1, 40000, 64, 17000, [20000, 40000, 100, 17001]), (3, 1, 8000, 128, 6000, [8000, 0, 6001])])
+def test_compact_long(dtype, b, H, P, dh, n, lens):
+    """Few heads with many kept keys: larger workgroups, and K in two launches; more places than keys."""
+    announce("compact long", dtype, b, H, P, dh, n, lens)
+    compact_case(dtype, b, H, P, dh, n, 3, lens=lens)
 
 
 def test_compact_indices_out_of_range_stay_inside():
