@@ -427,6 +427,7 @@ __device__ __forceinline__ uint32_t sum_rank(float w) {
 
 // HELD: the row's sums fit the registers (HELD keys a thread) and are read once; 0:
 // every pass reads them again, 16 keys a thread in flight.
+// A digit's bin that is taken whole ends the search.
 // BITS: of a digit; short rows take four of 8 bits in workgroups of 256 threads, whose
 // barriers are quick, others three of 11 in 1024.
 template <int THREADS, int HELD, int BITS>
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelectArgs a) {
     static_assert(BPT == 1 || BPT == 2, "a bin or two a thread");
     __shared__ uint32_t hist[COPIES][BINS];
     __shared__ uint32_t wsum[WAVES], wtie[WAVES];
-    __shared__ uint32_t found[2];
+    __shared__ uint32_t found[3];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = blockIdx.x / a.Hkv;
     const int p = prefix_len(a.prefix, s, a.P), m = min(a.n, p);
@@ -527,13 +528,22 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelectArgs a) {
         const uint32_t want = (uint32_t)need;
 #pragma unroll
         for (int i = 0; i < BPT; ++i) {
-            if (before < want && before + c[i] >= want) { found[0] = BINS - 1 - BPT * tid - i; found[1] = before; }
+            if (before < want && before + c[i] >= want) {
+                found[0] = BINS - 1 - BPT * tid - i;
+                found[1] = before;
+                found[2] = before + c[i] == want;
+            }
             before += c[i];
         }
         __syncthreads();
         T |= found[0] << shift;
         mask |= ((1u << bits) - 1) << shift;
         need -= (int)found[1];
+        if (found[2]) {                                      // the whole bin: all above T - 1, none that equals it
+            --T;
+            need = 0;
+            break;
+        }
     }
     // keys above T, and the first `need` of those that equal it, in index order
     uint32_t above = 0, ties = 0;
@@ -571,6 +581,82 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelectArgs a) {
             eq += u[e] == T;
         }
     });
+}
+
+// Short rows: one wave a row, no LDS and no barrier.  The threshold is found bit by bit
+// from the top, with a compare and a scalar count for every 64 keys, and the search ends
+// at the first bit that leaves exactly m keys at or above it.  (4096 rows of 500 sums 10
+// us, 8 of 300 5; a workgroup of 256 threads a row 16 and 5.5.  With 16 keys a lane the
+// counts take longer than histograms: 8 rows of 609 7.7 and 5.7.)
+constexpr int kWaveKeys = 8;                                 // of a lane
+
+__global__ __launch_bounds__(64) void kv_select_wave_kernel(KvSelectArgs a) {
+    constexpr int HELD = kWaveKeys;
+    const int lane = threadIdx.x, s = blockIdx.x / a.Hkv;
+    const int p = prefix_len(a.prefix, s, a.P), m = min(a.n, p);
+    const float* w = a.weights + (size_t)blockIdx.x * a.ldw;
+    int32_t* keep = a.keep + (size_t)blockIdx.x * a.n;
+    if (a.kept && blockIdx.x % a.Hkv == 0 && lane == 0) a.kept[s] = m;
+    for (int i = m + lane; i < a.n; i += 64) keep[i] = -1;
+    if (m == p) {                                            // nothing to leave out
+        for (int i = lane; i < m; i += 64) keep[i] = i;
+        return;
+    }
+    floatx4 x[HELD / 4];
+#pragma unroll
+    for (int i = 0; i < HELD / 4; ++i) {
+        const int j = 256 * i + 4 * lane;
+        x[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (j + 4 <= p) x[i] = ld_f4(w + j);
+        else if (j < p)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][e] = w[min(j + e, p - 1)];
+    }
+    uint32_t u[HELD];                                        // (0 past the last key: under every threshold but 0)
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int j = 256 * (i >> 2) + 4 * lane + (i & 3);
+        u[i] = j >= p ? 0u : j < a.first || j >= p - a.last ? 0xFFFFFFFFu : sum_rank(x[i >> 2][i & 3]);
+    }
+    // T: fewer than m keys rank above it, m or more at or above it
+    auto count = [&](uint32_t t) __attribute__((always_inline)) {
+        uint32_t c = 0;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) c += __builtin_popcountll(__ballot(u[i] >= t));
+        return c;
+    };
+    uint32_t T = 0, ties = 0;                                // ties: of the keys that equal T, how many to take
+    bool exact = false;
+    for (uint32_t bit = 0x80000000u; bit && !exact; bit >>= 1) {
+        const uint32_t c = count(T | bit);
+        if (c >= (uint32_t)m) T |= bit;
+        exact = c == (uint32_t)m;
+    }
+    if (exact) --T;                                          // all above T - 1, none of those that equal it
+    else ties = m - (T == 0xFFFFFFFFu ? 0u : count(T + 1));
+    uint32_t pos = 0, tie = 0;                               // keys above T, and ties, so far
+    const uint64_t lower = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < HELD; i += 4) {
+        const int j = 256 * (i >> 2) + 4 * lane;
+        uint32_t up = pos, eq = tie;                         // before this lane's four keys
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t ba = __ballot(u[i + e] > T), bt = __ballot(j + e < p && u[i + e] == T);
+            up += __builtin_popcountll(ba & lower);
+            eq += __builtin_popcountll(bt & lower);
+            pos += __builtin_popcountll(ba);
+            tie += __builtin_popcountll(bt);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = u[i + e];
+            if (j + e >= p) continue;
+            if (x > T || (x == T && eq < ties)) keep[up + min(eq, ties)] = j + e;
+            up += x > T;
+            eq += x == T;
+        }
+    }
 }
 
 // Long rows of few heads: every digit's histogram, and the indices, in a launch of
@@ -989,7 +1075,8 @@ hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s) {
         return hipSuccess;
     }
     const dim3 grid(a.b * a.Hkv);
-    if (a.P <= 2048) launch(kv_select_kernel<256, 8, 8>, grid, dim3(256), 0, s, a);
+    if (a.P <= 64 * kWaveKeys) launch(kv_select_wave_kernel, grid, dim3(64), 0, s, a);
+    else if (a.P <= 2048) launch(kv_select_kernel<256, 8, 8>, grid, dim3(256), 0, s, a);
     else if (a.P <= 8 * kSelThreads) launch(kv_select_kernel<kSelThreads, 8, 11>, grid, dim3(kSelThreads), 0, s, a);
     else if (a.P <= 16 * kSelThreads) launch(kv_select_kernel<kSelThreads, 16, 11>, grid, dim3(kSelThreads), 0, s, a);
     else launch(kv_select_kernel<kSelThreads, 0, 11>, grid, dim3(kSelThreads), 0, s, a);

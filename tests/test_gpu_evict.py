@@ -201,6 +201,20 @@ def test_select_ragged_and_strided():
     select_case(w, 100, 4, 16, lens=[50, 99, 299, 150, 7, 300, 20], ld=333)
 
 
+@pytest.mark.parametrize("P", [63, 256, 257, 511, 512, 513])
+def test_select_short(P):
+    """Rows at the sizes where a wave takes one, and next to them; keys at the threshold that are all taken, or not."""
+    announce("select short", P)
+    rng = np.random.default_rng(P)
+    select_case(rng.standard_normal((3, 5, P)).astype(np.float32), P // 2, 3, 9, ld=P + 1)
+    select_case(rng.integers(0, 4, (2, 2, P)).astype(np.float32), P // 3, 1, 1, lens=[P, P // 2])
+    w = np.zeros((1, 2, P), np.float32)
+    w[..., :7] = 1.0
+    for n in (6, 7, 8):                                              # one short of, all of, and one past equal sums
+        select_case(w, n)
+    select_case(w, 20, 10, 10)
+
+
 @pytest.mark.parametrize("n", [1, 20000, 45000])
 def test_select_long_ragged(n):
     """Rows of several workgroups whose lengths end at, and beside, the keys of one; more places than keys."""
