@@ -53,11 +53,13 @@ __device__ __forceinline__ uint64_t own_word(const uint64_t (&x)[kBlockWords], i
     return pre | bits64(x, B, s) | (~bits64(x, B, s - B) & range_mask(s - B, B));
 }
 
-// LDS: three K stages [64 keys][DH] and two V^T stages [DH][64 keys].
+// LDS: three K stages [64 keys][DH] and two V^T stages [DH][64 keys].  With two GROUPS of
+// waves each has stages, and a half of the workgroup's tiles, of its own, and the first
+// takes the second's results from LDS at the end: two waves a SIMD without a merge in memory.
 constexpr int kWaves = 4, kRows = 32 * kWaves;   // of a workgroup
 
-template <int DH, bool KV8>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2)))
+template <int DH, bool KV8, int GROUPS>
+__global__ __launch_bounds__(64 * kWaves * GROUPS) __attribute__((amdgpu_waves_per_eu(2)))
 void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     constexpr int ROWS = kRows, TILE = kKeys * DH * 2;
     constexpr int NI = kKeys * DH / 8 / (64 * kWaves);       // 16-byte chunks of a tile that a thread copies
@@ -65,9 +67,11 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     using KVT = typename std::conditional<KV8, uint8_t, bf16_t>::type;
     typedef __attribute__((address_space(3))) void* lds_ptr;
     typedef __attribute__((address_space(1))) void* glb_ptr;
-    __shared__ __attribute__((aligned(16))) char smem[5 * TILE];   // (and the rows' results on their way out)
+    __shared__ __attribute__((aligned(16))) char smem[GROUPS * 5 * TILE];   // (and the rows' results on their way out)
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = wid % kWaves, group = wid / kWaves;     // (of its group)
+    char* stages = smem + group * 5 * TILE;
     const int lr = lane & 31, eta = lane >> 5;
     // row tile fastest, then key split, then KV head, dealt to the XCDs in
     // contiguous runs: workgroups that read the same keys share an L2
@@ -96,7 +100,10 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
         if (lane >= o) upto += below;
     }
     const int ntiles = nsh + __builtin_amdgcn_readlane(upto, 63);
-    const int t_begin = (int)((long long)ntiles * split / nsplit), t_end = (int)((long long)ntiles * (split + 1) / nsplit);
+    auto first_of = [&](int part) __attribute__((always_inline)) { return (int)((long long)ntiles * part / (nsplit * GROUPS)); };
+    const int t_begin = first_of(split * GROUPS + group), t_end = first_of(split * GROUPS + group + 1);
+    int steps = t_end - t_begin;                             // (of the group that has more)
+    if constexpr (GROUPS == 2) steps = max(steps, first_of(split * 2 + 2 - group) - first_of(split * 2 + 1 - group));
     auto tile_at = [&](int t) __attribute__((always_inline)) {
         Tile d;
         if (t < nsh) {
@@ -254,8 +261,8 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
             }
         }
     };
-    auto kst = [&](int i) __attribute__((always_inline)) { return smem + (i % 3) * TILE; };
-    auto vst = [&](int i) __attribute__((always_inline)) { return smem + (3 + (i & 1)) * TILE; };
+    auto kst = [&](int i) __attribute__((always_inline)) { return stages + (i % 3) * TILE; };
+    auto vst = [&](int i) __attribute__((always_inline)) { return stages + (3 + (i & 1)) * TILE; };
     // tiles of this step, the next and the one after it (none: n = 0)
     const Tile none = {-1, 0, 0, 0};
     Tile t0 = t_begin < t_end ? tile_at(t_begin) : none, t1 = t_begin + 1 < t_end ? tile_at(t_begin + 1) : none;
@@ -460,7 +467,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     };
     // rows of this wave that the tile can concern
     auto concerns = [&](const Tile& t) __attribute__((always_inline)) {
-        return w_any && (t.seq < 0 || (t.seq >= w_lo && t.seq <= w_hi));
+        return w_any && (GROUPS == 1 || t.n) && (t.seq < 0 || (t.seq >= w_lo && t.seq <= w_hi));
     };
 
     // ---- main loop: V one step ahead of its use, K two.  A step ends by waiting for
@@ -470,7 +477,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     // than the count assumes, so then all are waited for.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    for (int it = 0; it < t_end - t_begin; ++it) {
+    for (int it = 0; it < steps; ++it) {
         const Tile t2 = t_begin + it + 2 < t_end ? tile_at(t_begin + it + 2) : none;
         if constexpr (KV8) {
             if (t1.n) load_v8(t1);
@@ -503,6 +510,33 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
         t1 = t2;
     }
 
+    // ---- the second group's results, through its stages, into the first's (lane by lane:
+    // both hold the same rows)
+    if constexpr (GROUPS == 2) {
+        constexpr int NO = DH / 8;                           // 16-byte pieces of a lane
+        char* at = smem + 5 * TILE + wave * NO * 1024 + lane * 16;
+        float2* ml = reinterpret_cast<float2*>(smem + 5 * TILE + kWaves * NO * 1024) + wave * 64 + lane;
+        if (group == 1) {
+#pragma unroll
+            for (int i = 0; i < NO; ++i)
+                *reinterpret_cast<floatx4*>(at + i * 1024) =
+                    floatx4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
+            *ml = make_float2(m_run, l_run);
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float2 v = *ml;
+        const float m_new = fmaxf(m_run, v.x), f0 = __builtin_amdgcn_exp2f(m_run - m_new), f1 = __builtin_amdgcn_exp2f(v.x - m_new);
+        m_run = m_new;
+        l_run = l_run * f0 + v.y * f1;
+#pragma unroll
+        for (int i = 0; i < NO; ++i) {
+            const floatx4 x = *reinterpret_cast<const floatx4*>(at + i * 1024);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i >> 2][4 * (i & 3) + e] = o[i >> 2][4 * (i & 3) + e] * f0 + x[e] * f1;
+        }
+    }
+
     // ---- epilogue: the two lanes of a row hold disjoint keys; a lane holds dims
     // 32 d + 8 j + 4 eta + {0..3}.  Rows go out through the wave's part of the LDS, so
     // that a store covers whole rows (16-byte pieces of 32 rows at a time took 7 us
@@ -511,7 +545,7 @@ void shared_attn_kernel(SharedAttnArgs a, int rowtiles, int nsplit) {
     const bool whole = nsplit == 1;
     const float inv = !whole ? 1.f : (l_tot == 0.f ? 0.f : 1.f / l_tot);   // (every score minus infinity: zeros)
     constexpr int FCH = DH / 4;                              // 16-byte chunks of a row in fp32
-    char* own = smem + wave * 32 * DH * 4;
+    char* own = stages + wave * 32 * DH * 4;
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -792,30 +826,44 @@ __global__ __launch_bounds__(64 * kWavesF) void shared_attn_f32_kernel(SharedAtt
 
 struct SharedCfg {
     int rowtiles, ns;
+    int groups;   // of waves in a workgroup (bf16, FP8)
 };
 
-// Key splits: the count of least estimated time.  A workgroup takes 5 us to start and
-// end and t us a tile (bf16: 1.6 alone on its CU, 2.4 for each of two; fp32: its four
-// waves a tile each in 2.5), a split 4 us for the merge and 1040 bytes a row written
-// and read at 5 TB/s.  Measured: 1024 rows x 32 heads, 36 tiles: 67 us whole, 66 in
-// two; 128 x 32, 28 tiles: 28 us in 7, 29 in 14; 16 x 32, 13 tiles: 14 us in 13, 17 in 6.
+// Key splits, and a second group of waves in every workgroup: what is least by estimate.
+// A step of a tile (fp32: of a tile for each of four waves) takes so many us for one
+// workgroup on a CU, for each of two, and for a pair of groups; a split 4 us for the merge
+// and 1040 bytes a row written and read at 5 TB/s, a second group 1.  So a pair is taken
+// where workgroups leave half of the chip empty and a merge would cost more than the steps
+// of two workgroups, which drift apart, save over those of a pair.  Measured (bf16; whole /
+// whole in pairs / in two splits): 1024 rows x 32 heads, 10 tiles 38 / 34 / 46 us, 30 tiles
+// 62 / 53 / 62, 82 tiles 151 / 126 / 126, 254 tiles 445 / 388 / 363; FP8 57 / 42 / 55,
+// 99 / 71 / 81, 272 / 175 / 176, 661 / 459 / 445.  16 rows x 32 heads, 13 tiles: 14 us in 13
+// splits, 17 in 6.
 SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     SharedCfg c{};
     const long rows = (long)b * 2 * B * (Hq / Hkv), RS = 2L * B * (Hq / Hkv);
     const bool f32 = dtype == DARD_DTYPE_F32;
-    const long per = f32 ? 16 : kRows, keys = f32 ? kKeysF : kKeys, step = f32 ? kWavesF : 1;
+    const long per = f32 ? 16 : kRows, keys = f32 ? kKeysF : kKeys;
     c.rowtiles = (int)((rows + per - 1) / per);
-    const long wgs = (long)c.rowtiles * Hkv, fit = f32 ? 256 : 512;
+    const long wgs = (long)c.rowtiles * Hkv;
     const long seqs = std::min<long>(b, (per + RS - 1) / RS);
     const long tiles = ((long)Ps + keys - 1) / keys + seqs * (((long)P + 2 * B + keys - 1) / keys);
+    const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8;
+    const double alone = f32 ? 2.5 : kv8 ? 3.0 : 1.75, two = kv8 ? 3.3 : 2.7, pair = kv8 ? 3.55 : 3.0;
+    const long step = f32 ? kWavesF : 1, fit = f32 ? 256 : 512;
     double best = 0;
     for (long ns = 1; ns <= kMaxSplit && (ns == 1 || (ns * wgs <= fit && ns * step <= tiles)); ++ns) {
-        const double t = f32 ? 2.5 : ns * wgs <= 256 ? 1.6 : 2.4;
-        const double us = (double)((tiles + ns * step - 1) / (ns * step)) * t + (ns > 1 ? 4 + (double)ns * rows * Hkv * 0.00021 : 0);
+        const double us = (double)((tiles + ns * step - 1) / (ns * step)) * (f32 || ns * wgs <= 256 ? alone : two) +
+                          (ns > 1 ? 4 + (double)ns * rows * Hkv * 0.00021 : 0);
         if (ns == 1 || us < best) {
             best = us;
             c.ns = (int)ns;
         }
+    }
+    c.groups = 1;
+    if (!f32 && wgs <= 256 && tiles > 1 && (double)((tiles + 1) / 2) * pair + 1 < best) {
+        c.ns = 1;
+        c.groups = 2;
     }
     return c;
 }
@@ -836,7 +884,9 @@ static hipError_t launch_shared(int dtype, const SharedAttnArgs& a, hipStream_t 
         launch(shared_attn_f32_kernel<DH>, grid, dim3(64 * kWavesF), 0, s, a, c.rowtiles, c.ns);
     } else {
         const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8;
-        launch(kv8 ? shared_attn_kernel<DH, true> : shared_attn_kernel<DH, false>, grid, dim3(64 * kWaves), 0, s, a, c.rowtiles, c.ns);
+        void (*k)(SharedAttnArgs, int, int) = c.groups == 2 ? (kv8 ? shared_attn_kernel<DH, true, 2> : shared_attn_kernel<DH, false, 2>)
+                                                            : (kv8 ? shared_attn_kernel<DH, true, 1> : shared_attn_kernel<DH, false, 1>);
+        launch(k, grid, dim3(64 * kWaves * c.groups), 0, s, a, c.rowtiles, c.ns);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.ns == 1) return e;

@@ -33,6 +33,7 @@ class Case:
         self.q = rng.standard_normal((b, 2 * B, Hq, dh)) * qstd
         self.state, self.conf = E.block(b, B, seed)
         self.scale, self.flags = dh ** -0.5, 0
+        self.heads = range(Hq) if Hq < 32 else (0, Hq // 2 + 1, Hq - 1)   # that are looked at
 
     def device(self):
         self.t = {n: E.storage(x, self.dtype)[0].cuda() for n, x in self.raw.items()}
@@ -67,7 +68,7 @@ class Case:
         for s in range(self.b):
             p = self.Ps + self.first[s]
             seen = E.visible(self.state[s], self.conf[s], p, self.flags)
-            for h in range(self.Hq):
+            for h in self.heads:
                 k, v = self.keys(s, h // (self.Hq // self.Hkv))
                 rows = np.ones(2 * self.B, bool)
                 if bad is not None:
@@ -125,6 +126,45 @@ def test_key_splits(dtype, b, B, Ps, P, Hq, Hkv, dh):
     """Few rows and many keys: split over workgroups and merged; large scores, so that maxima move."""
     announce("shared attention splits", dtype, b, B, Ps, P, Hq, Hkv, dh)
     Case(dtype, b, B, Ps, P, Hq, Hkv, dh, seed=5, qstd=4.0).device().call().verify()
+
+
+# rows times KV heads enough that a merge in memory costs more than it saves, workgroups too few for two on a
+# compute unit, several tiles: two groups of waves in a workgroup
+PAIRS = [(5, 64, 300, 150, 32, 16, 128), (40, 8, 500, 60, 32, 16, 64), (6, 33, 321, 0, 48, 16, 64), (3, 100, 90, 333, 48, 16, 128)]
+
+
+@pytest.mark.parametrize("dtype", [E.BF16, E.FP8])
+@pytest.mark.parametrize("b,B,Ps,P,Hq,Hkv,dh", PAIRS)
+def test_two_groups(dtype, b, B, Ps, P, Hq, Hkv, dh):
+    announce("shared attention groups", dtype, b, B, Ps, P, Hq, Hkv, dh)
+    assert dard.dard_attention_shared_workspace_bytes(DT[dtype], b, B, Hq, Hkv, dh, Ps, P) < b * 2 * B * Hq * (dh + 2) * 4   # no split
+    Case(dtype, b, B, Ps, P, Hq, Hkv, dh, seed=12, qstd=3.0).device().call().verify()
+    lens = [(61 * i) % (P + 1) for i in range(b)]    # 0 first: a group may have a tile less, or the rows of a wave none
+    Case(dtype, b, B, Ps, P, Hq, Hkv, dh, lens=lens, seed=13).device().call().verify()
+
+
+@pytest.mark.parametrize("dtype,what", [(E.BF16, float("inf")), (E.BF16, float("nan")), (E.FP8, float("nan"))])
+def test_two_groups_hidden_infinities(dtype, what):
+    test_hidden_infinities(dtype, what, 5, 64, 300, 150, 32, 16, 128)
+
+
+def test_two_groups_far_scores():
+    """One group sees only scores that the other's dwarf, or that are all minus infinity."""
+    announce("shared attention groups far scores")
+    c = Case(E.BF16, 5, 64, 300, 150, 32, 16, 128, seed=14)
+    c.raw["ksh"] *= 40.0
+    c.device().call().verify()
+    c = Case(E.BF16, 5, 64, 300, 150, 32, 16, 128, seed=14).device()
+    c.t["ksh"][..., 0], c.tq[..., 0] = float("-inf"), 1.0
+    c.call()
+    got, lse = c.out.clone(), c.lse.clone()
+    c = Case(E.BF16, 5, 64, 300, 150, 32, 16, 128, seed=14).device()
+    c.Ps, c.tq[..., 0] = 0, 1.0
+    c.call()
+    # (the same sums in another order, probabilities against another maximum: two roundings of 2^-8 each of a sum whose
+    # terms' magnitudes stay under 4, and 2^-8 of the result twice)
+    assert torch.all((got.float() - c.out.float()).abs() <= 2.0 ** -6 * 4) and torch.all((lse - c.lse).abs() <= 2.0 ** -12 * 16)
+    assert torch.isfinite(got).all()
 
 
 @pytest.mark.parametrize("dtype,what", [(E.BF16, float("inf")), (E.BF16, float("nan")), (E.F32, float("-inf")),
