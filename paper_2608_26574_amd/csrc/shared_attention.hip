@@ -838,7 +838,7 @@ struct SharedCfg {
 // whole in pairs / in two splits): 1024 rows x 32 heads, 10 tiles 38 / 34 / 46 us, 30 tiles
 // 62 / 53 / 62, 82 tiles 151 / 126 / 126, 254 tiles 445 / 388 / 363; FP8 57 / 42 / 55,
 // 99 / 71 / 81, 272 / 175 / 176, 661 / 459 / 445.  16 rows x 32 heads, 13 tiles: 14 us in 13
-// splits, 17 in 6.
+// splits, 17 in 6; fp32, 128 rows x 4 heads, 19 tiles: 11 us in 5 splits, 14 in 3, 20 whole.
 SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     SharedCfg c{};
     const long rows = (long)b * 2 * B * (Hq / Hkv), RS = 2L * B * (Hq / Hkv);
@@ -852,8 +852,9 @@ SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     const double alone = f32 ? 2.5 : kv8 ? 3.0 : 1.75, two = kv8 ? 3.3 : 2.7, pair = kv8 ? 3.55 : 3.0;
     const long step = f32 ? kWavesF : 1, fit = f32 ? 256 : 512;
     double best = 0;
-    for (long ns = 1; ns <= kMaxSplit && (ns == 1 || (ns * wgs <= fit && ns * step <= tiles)); ++ns) {
-        const double us = (double)((tiles + ns * step - 1) / (ns * step)) * (f32 || ns * wgs <= 256 ? alone : two) +
+    for (long ns = 1; ns <= kMaxSplit && (ns == 1 || (ns * wgs <= fit && (ns - 1) * step < tiles)); ++ns) {
+        const long most = (tiles + ns - 1) / ns;             // of a split
+        const double us = (double)((most + step - 1) / step) * (f32 || ns * wgs <= 256 ? alone : two) +
                           (ns > 1 ? 4 + (double)ns * rows * Hkv * 0.00021 : 0);
         if (ns == 1 || us < best) {
             best = us;
