@@ -630,10 +630,11 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  *   dard_kv_compact  key j of every (s, g) becomes key keep[s][g][j], j < m =
  *     kept[s] (NULL: n; at most n and p), in K, V and, when not NULL, weights, in
  *     place; weights m .. p - 1 become 0, so that keys written there start from
- *     nothing; every other key keeps its bytes.  keep ascends, as dard_kv_select
- *     writes it (indices are clamped into [0, p); other orders give unspecified
- *     keys).  With kept as the prefix of the next call, the block or new keys
- *     follow at m.  Needs P <= cap, at most 2^30.
+ *     nothing; every other key keeps its bytes.  keep ascends, no index twice, as
+ *     dard_kv_select writes it (indices are clamped into [0, p); other orders give
+ *     unspecified keys); a leading run of keys that keep their places is not moved.
+ *     With kept as the prefix of the next call, the block or new keys follow at m.
+ *     Needs P <= cap, at most 2^30.
  *
  * Workspaces (device, caller-owned, 16-byte aligned, contents need no
  * initialisation) by the queries; 0: none is needed, ws may be NULL. */

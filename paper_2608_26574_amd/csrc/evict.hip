@@ -837,6 +837,19 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArg
 // then writes that run, which no later chunk reads.  A workgroup owns whole
 // columns (a run of a key's bytes, or rows of the dims-major V), so the order of
 // reads and writes is its own affair.
+// Sources ascend, so keep[j] = j for a leading run of places and for no other: how many
+// whole chunks of it need no move (64 probes a step).
+__device__ __forceinline__ int chunks_in_place(const int32_t* keep, int m, int chunk) {
+    int n = 0;
+    for (;;) {
+        const long long end = min((long long)(n + (int)(threadIdx.x & 63) + 1) * chunk, (long long)m);
+        const uint64_t moved = __ballot(keep[end - 1] != (int)end - 1);
+        if (moved) return n + __builtin_ctzll(moved);
+        n += 64;
+        if ((long long)n * chunk >= m) return n;
+    }
+}
+
 // The waits below count operations: what is written before stays before.
 __device__ __forceinline__ void in_order() {
     asm volatile("" ::: "memory");
@@ -864,10 +877,14 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
         for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4*>(k + (size_t)src[u] * row_bytes + at);
     };
     indices(0);
+    const int at0 = chunks_in_place(keep, m, U * STEP);
+    if ((long long)at0 * U * STEP >= m) return;
+    const int first = at0 * U * STEP;
+    if (first) indices(first);
     load();
     in_order();
-    indices(U * STEP);
-    for (int j0 = 0; j0 < m; j0 += U * STEP) {
+    indices(first + U * STEP);
+    for (int j0 = first; j0 < m; j0 += U * STEP) {
         if (NEAR && keep[j0] >= m) break;
         u32x4 y[U];
 #pragma unroll
@@ -934,10 +951,14 @@ __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, 
                 for (int d = 0; d < ROWS; ++d) x[d][e][i] = v[(size_t)d * cap + src[e][i]];
     };
     indices(0);
+    const int at0 = chunks_in_place(keep, m, CHUNK);
+    if ((long long)at0 * CHUNK >= m) return;
+    const int first = at0 * CHUNK;
+    if (first) indices(first);
     load();
     in_order();
-    indices(CHUNK);
-    for (int j0 = 0; j0 < m; j0 += CHUNK) {
+    indices(first + CHUNK);
+    for (int j0 = first; j0 < m; j0 += CHUNK) {
         uint32_t y[ROWS][E];
 #pragma unroll
         for (int d = 0; d < ROWS; ++d)

@@ -225,7 +225,7 @@ def test_select_long_ragged(n):
 
 
 # ------------------------------------------------------------------ compaction
-def compact_case(dtype, b, H, P, dh, n, extra=0, lens=None, kept=True, sums=True, seed=0):
+def compact_case(dtype, b, H, P, dh, n, extra=0, lens=None, kept=True, sums=True, seed=0, stay=0):
     rng = np.random.default_rng(seed + P + n)
     cap = P + extra
     prefix, count = lengths(lens, b, P)
@@ -240,6 +240,9 @@ def compact_case(dtype, b, H, P, dh, n, extra=0, lens=None, kept=True, sums=True
         for h in range(H):
             m = min(n, p)
             keep[s, h, :m] = np.sort(rng.permutation(p)[:m])
+            if stay:                                                 # the first keys stay where they are
+                i = min(stay, m)
+                keep[s, h, :m] = np.concatenate([np.arange(i), i + np.sort(rng.permutation(p - i)[:m - i])])
     tkept = torch.tensor([min(n, p) for p in count], dtype=torch.int32, device="cuda") if kept else None
     k0, v0, w0 = k.clone(), v.clone(), w.clone()
     dard.dard_kv_compact(k.view(t), v.view(t), dev(keep), P, weights=w if sums else None, kept=tkept, prefix=prefix)
@@ -279,6 +282,15 @@ def test_compact_long(dtype, b, H, P, dh, n, lens):
     """Few heads with many kept keys: larger workgroups, and K in two launches; more places than keys."""
     announce("compact long", dtype, b, H, P, dh, n, lens)
     compact_case(dtype, b, H, P, dh, n, 3, lens=lens)
+
+
+@pytest.mark.parametrize("dtype", [E.BF16, E.FP8, E.F32])
+@pytest.mark.parametrize("b,H,P,dh,n", [(2, 2, 3000, 64, 2100), (1, 1, 12000, 128, 9000), (1, 1, 40000, 64, 20000)])
+def test_compact_keys_that_stay(dtype, b, H, P, dh, n):
+    """A leading run of keys keeps its places: runs that end at, and beside, the chunks of a pass, and everywhere else."""
+    announce("compact stay", dtype, b, H, P, dh, n)
+    for stay in (1, 255, 256, 511, 512, 513, 1024, 2047, 2048, 4095, 4096, 4097, 8192, n - 1, n):
+        compact_case(dtype, b, H, P, dh, n, 1, stay=stay)
 
 
 def test_compact_indices_out_of_range_stay_inside():
