@@ -120,6 +120,22 @@ def test_mask_flags(dtype, flags):
     c.device().call().verify()
 
 
+FLAGS = [0, O.F_XSELF_SHADOW, O.F_MKEYS_SHADOW, O.F_C_BIDIR, O.F_ORDER_L2R, O.F_C_BIDIR | O.F_XSELF_SHADOW,
+         O.F_XSELF_SHADOW | O.F_MKEYS_SHADOW | O.F_ORDER_L2R]
+
+
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("b,B,Hq,Hkv", [(9, 1, 2, 2), (9, 2, 3, 1), (7, 5, 2, 2), (5, 15, 2, 2), (5, 16, 2, 2), (4, 17, 2, 2), (4, 31, 2, 1), (3, 32, 2, 2),
+                                        (2, 33, 2, 2)])
+def test_mask_of_few_positions(b, B, Hq, Hkv, flags):
+    """Blocks whose mask the kernel works out by itself, waves that hold rows of several sequences; equal confidences."""
+    announce("shared attention few positions", b, B, Hq, Hkv, flags)
+    c = Case(E.BF16, b, B, 20, 10, Hq, Hkv, 64, lens=[(7 * i) % 11 for i in range(b)], seed=15)
+    c.flags = flags
+    c.conf[:, ::3] = c.conf[0, 0]
+    c.device().call().verify()
+
+
 @pytest.mark.parametrize("dtype", [E.BF16, E.FP8, E.F32])
 @pytest.mark.parametrize("b,B,Ps,P,Hq,Hkv,dh", [(2, 1, 4000, 9, 2, 2, 128), (16, 1, 3000, 65, 1, 1, 64), (3, 9, 1500, 10, 7, 1, 128)])
 def test_key_splits(dtype, b, B, Ps, P, Hq, Hkv, dh):
