@@ -422,7 +422,7 @@ WeightCfg weight_cfg(int dtype, int b, int R, int Hq, int Hkv, int P) {
 // consecutive keys, counts what it keeps, and writes its indices behind those of
 // the waves before it.  Bound by the chain of barriers and histogram counts, not by
 // bytes: 8 rows of 609 sums 5.7 us, 512 of 1664 8.8, 4 of 131072 (several workgroups a
-// row) 34 in four launches.
+// row) 32 in four launches.
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
 __device__ __forceinline__ uint32_t sum_rank(float w) {
@@ -556,10 +556,15 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelectArgs a) {
     run([&](const uint32_t (&u)[4], int j) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            above += __builtin_popcountll(__ballot(j + e < j1 && u[e] > T));
-            ties += __builtin_popcountll(__ballot(j + e < j1 && u[e] == T));
+            above += j + e < j1 && u[e] > T;
+            ties += j + e < j1 && u[e] == T;
         }
     });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        above += __shfl_xor(above, o, 64);
+        ties += __shfl_xor(ties, o, 64);
+    }
     if (lane == 0) { wsum[wave] = above; wtie[wave] = ties; }
     __syncthreads();
     uint32_t pos = 0, tie = 0;                               // keys above T, and ties, before this wave's run
@@ -674,14 +679,16 @@ __global__ __launch_bounds__(64) void kv_select_wave_kernel(KvSelectArgs a) {
 constexpr int kChunkKeys = 16;                               // keys a thread
 constexpr int kChunk = kSelThreads * kChunkKeys, kBins = 2048;
 
-__global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArgs a, int chunks, int digit) {
+template <int digit>
+__global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArgs a, int chunks) {
     constexpr int COPIES = 4;                                // (by lane, as in kv_select_kernel)
     __shared__ uint32_t hist[COPIES][kBins];
     __shared__ uint32_t wsum[kSelWaves], wtie[kSelWaves];
     __shared__ uint32_t found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x / chunks, chunk = blockIdx.x % chunks, s = row / a.Hkv;
-    const int p = prefix_len(a.prefix, s, a.P), m = min(a.n, p), last = digit == 3;
+    const int p = prefix_len(a.prefix, s, a.P), m = min(a.n, p);
+    constexpr bool last = digit == 3;
     int32_t* keep = a.keep + (size_t)row * a.n;
     const int c0 = chunk * kChunk;
     if (last) {
@@ -719,15 +726,22 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArg
     uint32_t* counts = state + (size_t)6 * rows;
     uint32_t T = 0, mask = 0, pos = 0, tie = 0;              // pos, tie: keys above T, and ties, of the chunks before this one
     int need = m;
+    // what the launches before left, on its way together
+    uint2 left[2] = {};
+    uint32_t before0 = 0;
+#pragma unroll
+    for (int d = 0; d + 1 < digit; ++d) {
+        left[d] = reinterpret_cast<const uint2*>(state)[(size_t)d * rows + row];
+        if (last)
+            for (int c = lane; c < chunk; c += 64) before0 += counts[((size_t)d * rows + row) * chunks + c];
+    }
+#pragma unroll
     for (int d = 0; d < digit; ++d) {
         const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bits = d == 2 ? 10 : 11;
         uint32_t bin, over;
         if (d + 1 < digit) {
-            const uint2 v = reinterpret_cast<const uint2*>(state)[(size_t)d * rows + row];
-            bin = v.x;
-            over = v.y;
-            if (last)
-                for (int c = 0; c < chunk; ++c) pos += counts[((size_t)d * rows + row) * chunks + c];
+            bin = left[d].x;
+            over = left[d].y;
         } else {
             // this thread's two bins, from the top; their counts in this chunk and in those before it
             const uint32_t* h = a.ws + ((size_t)d * gridDim.x + (size_t)row * chunks) * kBins + 2046 - 2 * tid;
@@ -774,7 +788,9 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArg
 #pragma unroll
             for (int i = 0; i < kSelWaves; ++i) { up += wsum[i]; eq += wtie[i]; }
             if (last) {
-                pos += up;
+#pragma unroll
+                for (int o = 32; o > 0; o >>= 1) before0 += __shfl_xor(before0, o, 64);
+                pos = up + before0;
                 tie = eq;
             } else if (tid == 0) {
                 counts[((size_t)d * rows + row) * chunks + chunk] = up;
@@ -799,15 +815,14 @@ __global__ __launch_bounds__(kSelThreads) void kv_select_long_kernel(KvSelectArg
         for (int i = 0; i < kBins; i += kSelThreads) h[i + tid] = hist[0][i + tid] + hist[1][i + tid] + hist[2][i + tid] + hist[3][i + tid];
         return;
     }
-    // this chunk's waves before this one
-    uint32_t mine = 0, eq = 0;
+    // this chunk's waves before this one (counts of a wave are under 2^16: two in a register)
+    uint32_t mine = 0;
 #pragma unroll
-    for (int i = 0; i < kChunkKeys; ++i) {
-        mine += __builtin_popcountll(__ballot(in[i] && u[i] > T));
-        eq += __builtin_popcountll(__ballot(in[i] && u[i] == T));
-    }
+    for (int i = 0; i < kChunkKeys; ++i) mine += in[i] ? (u[i] > T ? 1u : 0u) + (u[i] == T ? 1u << 16 : 0u) : 0u;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
     __syncthreads();
-    if (lane == 0) { wsum[wave] = mine; wtie[wave] = eq; }
+    if (lane == 0) { wsum[wave] = mine & 0xFFFFu; wtie[wave] = mine >> 16; }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSelWaves; ++i) {
@@ -1097,8 +1112,10 @@ size_t kv_select_workspace(int b, int Hkv, int P) {
 hipError_t launch_kv_select(const KvSelectArgs& a, hipStream_t s) {
     const int chunks = select_chunks(a.b, a.Hkv, a.P);
     if (chunks > 1) {
-        for (int digit = 0; digit <= 3; ++digit) {
-            launch(kv_select_long_kernel, dim3((unsigned)((long)a.b * a.Hkv * chunks)), dim3(kSelThreads), 0, s, a, chunks, digit);
+        void (*const digits[])(KvSelectArgs, int) = {kv_select_long_kernel<0>, kv_select_long_kernel<1>, kv_select_long_kernel<2>,
+                                                     kv_select_long_kernel<3>};
+        for (auto k : digits) {
+            launch(k, dim3((unsigned)((long)a.b * a.Hkv * chunks)), dim3(kSelThreads), 0, s, a, chunks);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
