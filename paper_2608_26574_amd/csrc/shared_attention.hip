@@ -858,7 +858,8 @@ SharedCfg shared_cfg(int dtype, int b, int B, int Hq, int Hkv, int Ps, int P) {
     const long per = f32 ? 16 : kRows, keys = f32 ? kKeysF : kKeys;
     c.rowtiles = (int)((rows + per - 1) / per);
     const long wgs = (long)c.rowtiles * Hkv;
-    const long seqs = std::min<long>(b, (per + RS - 1) / RS);
+    // sequences among a workgroup's rows, at most (they may begin inside it)
+    const long seqs = std::min<long>(b, per % RS == 0 ? per / RS : RS % per == 0 ? 1 : (per - 2) / RS + 2);
     const long tiles = ((long)Ps + keys - 1) / keys + seqs * (((long)P + 2 * B + keys - 1) / keys);
     const bool kv8 = dtype == DARD_DTYPE_BF16_KV_FP8;
     const double alone = f32 ? 2.5 : kv8 ? 3.0 : 1.75, two = kv8 ? 3.3 : 2.7, pair = kv8 ? 3.55 : 3.0;
