@@ -874,10 +874,20 @@ __device__ __forceinline__ int chunks_in_place(const int32_t* keep, int m, int c
     }
 }
 
-// The waits below count operations: what is written before stays before.
+// What is written before stays before.
 __device__ __forceinline__ void in_order() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
+}
+
+// Every source of a chunk that any wave has asked for is in registers: only then is the
+// chunk written.  (All loads and stores are waited for, not a count of the newer ones: that
+// would rest on the order and the number of instructions that the compiler makes of them.  The
+// indices of the next chunk, which are newer than its sources, are waited for here in any case.)
+__device__ __forceinline__ void sources_read() {
+    in_order();
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    wg_barrier();
 }
 
 // A workgroup owns SEG bytes of every key; a thread moves 16 bytes at a time, the
@@ -913,10 +923,7 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
         u32x4 y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) y[u] = x[u];
-        // every source of the chunk is in registers; the last chunk's stores, or the first
-        // indices, which are newer, may still be under way
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(U));
-        wg_barrier();
+        sources_read();
         if (j0 + U * STEP < m) load();
         indices(j0 + 2 * U * STEP);
 #pragma unroll
@@ -948,10 +955,10 @@ __device__ __forceinline__ void move_far_keys(char* k, int row_bytes, const int3
 // A workgroup owns ROWS rows of `cap` elements; a thread takes the elements of 4
 // bytes of a row at a time: their sources lie close together (the share of keys
 // that is kept apart), so single loads reach whole lines between a wave's lanes.
-template <typename T> struct Word;   // 4 bytes at an element's alignment
-template <> struct Word<float> { typedef uint32_t type; };
-template <> struct Word<uint16_t> { typedef uint32_t type __attribute__((aligned(2))); };
-template <> struct Word<uint8_t> { typedef uint32_t type __attribute__((aligned(1))); };
+template <typename T> struct Word;   // 4 bytes at an element's alignment, over elements that are loaded as T
+template <> struct Word<float> { typedef uint32_t type __attribute__((may_alias)); };
+template <> struct Word<uint16_t> { typedef uint32_t type __attribute__((aligned(2), may_alias)); };
+template <> struct Word<uint8_t> { typedef uint32_t type __attribute__((aligned(1), may_alias)); };
 
 template <typename T, int THREADS, int ROWS, int E>
 __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, int m, int P) {
@@ -996,10 +1003,7 @@ __device__ __forceinline__ void move_values(T* v, int cap, const int32_t* keep, 
                     for (int i = 0; i < SU; ++i) y[d][e] |= (uint32_t)x[d][e][i] << (8 * (int)sizeof(T) * i);
                 }
             }
-        // every source of the chunk is in registers; the last chunk's stores, or the first
-        // indices, which are newer, may still be under way
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm(E * (SU < ROWS ? SU : ROWS)));
-        wg_barrier();
+        sources_read();
         if (j0 + CHUNK < m) load();
         indices(j0 + 2 * CHUNK);
 #pragma unroll
