@@ -594,7 +594,8 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  * dims-major [..][dh][cap]); q, out, K and V of the 16- and 8-bit types are 16-byte
  * aligned, everything else as its element.  Sequences may have prefixes of
  * different lengths: `prefix`, when not NULL, is a device array of b lengths,
- * clamped into [0, P]; NULL: P each.
+ * clamped into [0, P]; NULL: P each.  With P = 0 the caches and the sums of key
+ * weights, selection and compaction have no element and may be NULL.
  *
  *   dard_masked_attention_shared  dard_masked_attention with a prefix of Ps shared
  *     keys and then the sequence's own p = prefix[s] or P:

@@ -728,7 +728,7 @@ size_t dard_key_weights_workspace_bytes(int dtype, int b, int R, int Hq, int Hkv
 dard_status dard_key_weights(int dtype, const void* q, const float* lse, const void* k, int P, const int32_t* prefix,
                              int cap, int b, int R, int Hq, int Hkv, int dh, float scale, float decay, float* weights,
                              int64_t ldw, void* ws, size_t ws_bytes, void* stream) {
-    if (!q || !lse || !k || !weights) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (!q || !lse || (P != 0 && (!k || !weights))) return fail(DARD_ERR_ARG, "NULL pointer");
     if (int rc = check_scale(scale)) return rc;
     if (!(decay >= 0.f && decay <= 1.f)) return fail(DARD_ERR_ARG, "need 0 <= decay <= 1");
     if (int rc = check_key_weights(dtype, b, R, Hq, Hkv, dh, P)) return rc;
@@ -765,7 +765,7 @@ size_t dard_kv_select_workspace_bytes(int b, int Hkv, int P, int n) {
 
 dard_status dard_kv_select(const float* weights, int64_t ldw, int P, const int32_t* prefix, int b, int Hkv, int n, int first,
                            int last, int32_t* keep, int32_t* kept, void* ws, size_t ws_bytes, void* stream) {
-    if (!weights || !keep) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (!keep || (P != 0 && !weights)) return fail(DARD_ERR_ARG, "NULL pointer");
     if (int rc = check_select(b, Hkv, P, n)) return rc;
     if (ldw < P) return fail(DARD_ERR_SHAPE, "P must be <= ldw");
     if (first < 0 || last < 0 || first > n || last > n - first)
@@ -786,7 +786,7 @@ dard_status dard_kv_select(const float* weights, int64_t ldw, int P, const int32
 
 dard_status dard_kv_compact(int dtype, void* k, void* v, int cap, float* weights, int64_t ldw, const int32_t* keep, int n,
                             const int32_t* kept, int P, const int32_t* prefix, int b, int Hkv, int dh, void* stream) {
-    if (!k || !v || !keep) return fail(DARD_ERR_ARG, "NULL pointer");
+    if (!keep || (P != 0 && (!k || !v))) return fail(DARD_ERR_ARG, "NULL pointer");
     if (int rc = check_kv_type(dtype)) return rc;
     if (int rc = check_heads(b, Hkv, Hkv, dh)) return rc;
     if (P < 0 || n < 1 || P > cap || (weights && ldw < P)) return fail(DARD_ERR_SHAPE, "need n >= 1 and 0 <= P <= cap, ldw");

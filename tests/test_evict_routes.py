@@ -1,6 +1,7 @@
 """Which kernels shared-prefix attention, key weights, selection and compaction launch, on the CPU: a small C library
 takes the place of the kernel start, writes down each kernel's name and grid, and nothing runs.  Every kernel of the two
 source files is started by some shape that the GPU tests run."""
+import ctypes
 import json
 import os
 import subprocess
@@ -53,7 +54,7 @@ for line in sys.stdin:
         rc = L.dard_key_weights(t, p, p, p, P, N, P, b, R, Hq, Hkv, dh, F(0.1), F(0.5), p, I64(P), p, room, N)
     elif what == "s":
         b, H, P, n = v
-        rc = L.dard_kv_select(p, I64(P), P, N, b, H, n, 0, 0, p, N, p, room, N)
+        rc = L.dard_kv_select(p if P else N, I64(P), P, N, b, H, n, 0, 0, p, N, p, room, N)
     elif what == "c":
         t, b, H, P, dh, n = v
         rc = L.dard_kv_compact(t, p, p, P, p, I64(P), p, n, N, P, N, b, H, dh, N)
@@ -169,3 +170,17 @@ def test_every_kernel_runs_in_a_test(routes):
     ran = {n for launches in routes(calls) for n, *_ in launches}
     there = {n for n, in routes([("list",)])[0] if "kv_select" in n or "kv_compact" in n or "key_weights" in n or "shared_attn" in n}
     assert len(there) > 40 and not there - ran, sorted(there - ran)
+
+
+def test_lengths_of_zero(routes):
+    """A cache and sums without a key are empty tensors, whose address is NULL: nothing to weigh or to move, and a selection
+    that writes -1 everywhere."""
+    (launches,) = routes([("s", 3, 2, 0, 5)])
+    assert len(launches) == 1 and launches[0][1] == 6
+    lib, some = dard.lib(), ctypes.c_void_p(1 << 20)
+    for dtype in DT.values():
+        assert lib.dard_key_weights(dtype, some, some, None, 0, None, 0, 1, 2, 4, 2, 64, 0.1, 0.5, None, 0, None, 0, None) == 0
+        assert lib.dard_kv_compact(dtype, None, None, 0, None, 0, some, 5, None, 0, None, 1, 2, 64, None) == 0
+        # (with a key they are asked for as ever)
+        assert lib.dard_key_weights(dtype, some, some, None, 1, None, 1, 1, 2, 4, 2, 64, 0.1, 0.5, some, 1, None, 0, None) == -1
+        assert lib.dard_kv_compact(dtype, some, None, 1, None, 0, some, 5, None, 1, None, 1, 2, 64, None) == -1

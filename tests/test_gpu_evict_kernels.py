@@ -132,3 +132,16 @@ def test_compact_few_heads_of_64(dtype, b, H, P, dh, n):
     compact_case(dtype, b, H, P, dh, n, 3)
     compact_case(dtype, b, H, P, dh, n, 1, lens=[P, n + 1][:b], stay=4097)
     compact_case(dtype, b, H, P, dh, n, 0, kept=False, sums=False, lens=[n - 1, P][:b])
+
+
+def test_lengths_of_zero():
+    """Empty caches and sums: nothing is weighed or moved, a selection takes no key."""
+    announce("eviction of nothing")
+    b, H, dh, n = 3, 2, 64, 5
+    q, lse = torch.ones(b, 4, 4, dh, device="cuda").bfloat16(), torch.zeros(b, 4, 4, device="cuda")
+    k, v, w = q.new_empty(b, H, 0, dh), q.new_empty(b, H, dh, 0), lse.new_empty(b, H, 0)
+    keep, kept = torch.full((b, H, n), 7, dtype=torch.int32, device="cuda"), torch.full((b,), 7, dtype=torch.int32, device="cuda")
+    dard.dard_key_weights(q, lse, k, 0, 0.125, 0.5, w)
+    dard.dard_kv_select(w, 0, keep, first=1, last=2, kept=kept)
+    dard.dard_kv_compact(k, v, keep, 0, weights=w, kept=kept)
+    assert torch.all(keep == -1) and torch.all(kept == 0)
