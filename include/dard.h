@@ -57,8 +57,8 @@ typedef int dard_status;
 
 /* Storage types of weights / activations / KV cache.  Logits, confidences
  * and the residual stream are always float32.  DARD_DTYPE_BF16_KV_FP8 is an
- * operation type of dard_masked_attention only: bf16 q / out with K and V in
- * OCP FP8 E4M3. */
+ * operation type of dard_masked_attention and of the shared-prefix and eviction
+ * calls only: bf16 q / out with K and V in OCP FP8 E4M3. */
 #define DARD_DTYPE_F32  0
 #define DARD_DTYPE_BF16 1
 #define DARD_DTYPE_BF16_KV_FP8 2
@@ -610,6 +610,8 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  *     bf16 (bf16, FP8 caches), sums and statistics are float32.  What stands in
  *     keys that a row does not see, also infinities and NaN, does not reach it; a
  *     row whose scores are all minus infinity gives zeros and lse = minus infinity.
+ *     Scores are taken times log2 e in float32: one that passes float32 there (from
+ *     2.3e38 on) counts as infinite.  The same in dard_key_weights, for lse too.
  *
  *   dard_key_weights  for every prefix key j < p of every KV head g
  *       weights[s][g][j] = decay weights[s][g][j] +
@@ -635,6 +637,11 @@ dard_status dard_masked_attention_mx(const void* q, const void* kc, const uint8_
  *     dard_kv_select writes it (indices are clamped into [0, p); other orders give
  *     unspecified keys); a leading run of keys that keep their places is not moved.
  *     With kept as the prefix of the next call, the block or new keys follow at m.
+ *     That is their place in the cache, not their position: kept keys keep the
+ *     rotary positions that they were written with, and the block goes on at its
+ *     own, which the caller applies to q and k.  dard_prefill, dard_step and their
+ *     variants count positions from the prefix length and take one length for all
+ *     sequences, so they do not continue from a cut cache.
  *     Needs P <= cap, at most 2^30.
  *
  * Workspaces (device, caller-owned, 16-byte aligned, contents need no

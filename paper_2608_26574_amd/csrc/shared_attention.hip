@@ -26,7 +26,10 @@
 // shared and up to 256 own keys 0.49 ms, 995 TFLOP/s: the matrix unit is busy in 48 % of a
 // SIMD's cycles, vector instructions issue in 40 %.  128 rows x 32 heads, 32768 shared keys
 // 158 us, 537 MB of K and V at 3.4 TB/s: 16 splits, two workgroups a CU, that wait for
-// their tiles.
+// their tiles.  The same from an FP8 cache takes longer, 207 us for half the bytes: codes go
+// through registers, V chunks by the path for a cache's end in every tile, and are widened
+// between the products and the barrier.  Heads of 64: 4096 rows x 4 heads, 8192 shared and up
+// to 256 own keys 68 us (FP8 87), 26 at the matrix unit's full rate.
 #include <algorithm>
 #include <type_traits>
 
@@ -649,7 +652,9 @@ __global__ __launch_bounds__(256) void shared_attn_combine_kernel(const float* _
 // space; its four waves take interleaved tiles of 32 keys, shared ones first, and
 // merge through LDS in wave order.  S^T = K Q^T leaves lane l (token l % 16, g = l / 16)
 // with keys 4g .. 4g + 3, and the B operand of step e of O^T += V^T P^T is key
-// 4g + e, so probabilities are used where they are.
+// 4g + e, so probabilities are used where they are.  K and V are loaded where they are used,
+// by a single wave a SIMD: 256 rows x 32 heads of 128, 2048 shared and up to 128 own keys 170 us
+// (59 at the matrix unit's full rate); 2048 rows x 4 heads of 64, 4096 and up to 128 134 (58).
 constexpr int kWavesF = 4, kKeysF = 32;
 
 template <int DH>
@@ -846,7 +851,8 @@ struct SharedCfg {
 // workgroup on a CU, for each of two, and for a pair of groups; a split 4 us for the merge
 // and 1040 bytes a row written and read at 5 TB/s, a second group 1.  So a pair is taken
 // where workgroups leave half of the chip empty and a merge would cost more than the steps
-// of two workgroups, which drift apart, save over those of a pair.  Measured (bf16; whole /
+// of two workgroups, which drift apart, save over those of a pair.  The constants are of heads
+// of 128 and stand for 64 too (unmeasured there).  Measured (bf16; whole /
 // whole in pairs / in two splits): 1024 rows x 32 heads, 10 tiles 38 / 34 / 46 us, 30 tiles
 // 62 / 53 / 62, 82 tiles 151 / 126 / 126, 254 tiles 445 / 388 / 363; FP8 57 / 42 / 55,
 // 99 / 71 / 81, 272 / 175 / 176, 661 / 459 / 445.  16 rows x 32 heads, 13 tiles: 14 us in 13
