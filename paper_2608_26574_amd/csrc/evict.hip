@@ -16,6 +16,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4e __attribute__((aligned(4)));            // at an fp32 element's alignment
 
 __device__ __forceinline__ int prefix_len(const int32_t* prefix, int s, int P) {
     return prefix ? min(max(prefix[s], 0), P) : P;
@@ -912,7 +913,7 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
     };
     auto load = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4*>(k + (size_t)src[u] * row_bytes + at);
+        for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const u32x4e*>(k + (size_t)src[u] * row_bytes + at);
     };
     indices(0);
     const int at0 = chunks_in_place(keep, m, U * STEP);
@@ -933,7 +934,7 @@ __device__ __forceinline__ void move_keys(char* k, int row_bytes, const int32_t*
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * STEP + key;
-            if (j < m && (!NEAR || keep[j] < m)) *reinterpret_cast<u32x4*>(k + (size_t)j * row_bytes + at) = y[u];
+            if (j < m && (!NEAR || keep[j] < m)) *reinterpret_cast<u32x4e*>(k + (size_t)j * row_bytes + at) = y[u];
         }
     }
 }
@@ -949,11 +950,11 @@ __device__ __forceinline__ void move_far_keys(char* k, int row_bytes, const int3
     for (int u = 0; u < U; ++u) {
         const int j = j0 + u * step + (int)threadIdx.x / lpr, src = keep[min(j, m - 1)];
         far[u] = j < m && src >= m;
-        x[u] = *reinterpret_cast<const u32x4*>(k + (size_t)min(max(src, 0), P - 1) * row_bytes + at);
+        x[u] = *reinterpret_cast<const u32x4e*>(k + (size_t)min(max(src, 0), P - 1) * row_bytes + at);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (far[u]) *reinterpret_cast<u32x4*>(k + (size_t)(j0 + u * step + threadIdx.x / lpr) * row_bytes + at) = x[u];
+        if (far[u]) *reinterpret_cast<u32x4e*>(k + (size_t)(j0 + u * step + threadIdx.x / lpr) * row_bytes + at) = x[u];
 }
 
 // A workgroup owns ROWS rows of `cap` elements; a thread takes the elements of 4
