@@ -145,3 +145,51 @@ def test_lengths_of_zero():
     dard.dard_kv_select(w, 0, keep, first=1, last=2, kept=kept)
     dard.dard_kv_compact(k, v, keep, 0, weights=w, kept=kept)
     assert torch.all(keep == -1) and torch.all(kept == 0)
+
+
+def test_long_eviction_captured():
+    """Key weights of two blocks a wave, a selection in four launches and a compaction in two, captured and replayed between
+    eager calls that share the workspaces, on a stream of the caller's: every replay gives the eager call's bits."""
+    announce("long eviction captured")
+    b, H, P, dh, n, R = 1, 4, 40000, 64, 17000, 300
+    g = torch.Generator(device="cuda").manual_seed(41)
+    q = torch.randn(b, R, 2 * H, dh, generator=g, device="cuda").bfloat16()
+    k0 = torch.randn(b, H, P, dh, generator=g, device="cuda").bfloat16()
+    v0 = torch.randn(b, H, dh, P, generator=g, device="cuda").bfloat16()
+    lse, k, v = torch.full((b, R, 2 * H), 10.0, device="cuda"), k0.clone(), v0.clone()
+    w, kept = torch.zeros(b, H, P, device="cuda"), torch.zeros(b, dtype=torch.int32, device="cuda")
+    keep = torch.zeros(b, H, n, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([39000], dtype=torch.int32, device="cuda")
+    rooms = [torch.empty(x + 16, dtype=torch.uint8, device="cuda") for x in (
+        dard.dard_key_weights_workspace_bytes(dard.DTYPE_BF16, b, R, 2 * H, H, dh, P), dard.dard_kv_select_workspace_bytes(b, H, P, n))]
+
+    def evict(stream=None):
+        dard.dard_key_weights(q, lse, k, P, 0.125, 0.0, w, ws=rooms[0], prefix=lens, stream=stream)
+        dard.dard_kv_select(w, P, keep, first=3, last=5, kept=kept, ws=rooms[1], prefix=lens, stream=stream)
+        dard.dard_kv_compact(k, v, keep, P, weights=w, kept=kept, prefix=lens, stream=stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    evict(side)
+    side.synchronize()
+    want = [t.clone() for t in (k, v, w, keep, kept)]
+    at = keep[0, :, :, None].long()
+    assert torch.equal(k[0, :, :n], k0[0].gather(1, at.expand(H, n, dh)))
+    assert torch.equal(v[0, :, :, :n], v0[0].gather(2, keep[0, :, None].long().expand(H, dh, n)))
+    k.copy_(k0), v.copy_(v0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        evict()
+    for i in range(3):
+        k.copy_(k0), v.copy_(v0), w.fill_(float(i)), keep.fill_(i), kept.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        # (sums past the sequence's length keep their values)
+        assert all(torch.equal(x, y) for x, y in zip((k, v, keep, kept), (want[0], want[1], want[3], want[4])))
+        assert torch.equal(w[..., :39000], want[2][..., :39000]) and torch.all(w[..., 39000:] == i)
+        for room in rooms:
+            room.fill_(0xA5)
+        k.copy_(k0), v.copy_(v0)
+        evict()
+        torch.cuda.synchronize()
+        assert torch.equal(k, want[0]) and torch.equal(keep, want[3])
